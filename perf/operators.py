@@ -151,7 +151,7 @@ def _encode(x):
     magnitude, a code the nearest magnitude, ties to the even code."""
     g = x.float().unflatten(-1, (-1, GROUP))
     m, e = torch.frexp(g.abs().amax(-1))
-    e = torch.where(m > 0, e - 3 + (m >= 0.875), -127).clamp(-127, 126)
+    e = torch.where(m > 0, e - 3 + (m >= 0.875), -127).clamp(-127, 125)
     y = g.abs() * ((127 - e) << 23).view(torch.float32).unsqueeze(-1)
     code = ((y > 0.25).to(torch.uint8) + (y >= 0.75) + (y > 1.25) + (y >= 1.75) + (y > 2.5) + (y >= 3.5) + (y > 5.0))
     code = (code + 8 * torch.signbit(g)).to(torch.uint8).flatten(-2).unflatten(-1, (-1, 2))
