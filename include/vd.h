@@ -317,6 +317,158 @@ size_t vd_evict_step_split_size(const vd_cache_desc *desc);
 /* Bytes of device workspace vd_evict_step needs for this descriptor (0 in this build). */
 size_t vd_evict_step_workspace_size(const vd_cache_desc *desc);
 
+/* ---------------------------------------------------------------------------
+ * A KV cache held in 4 bits.
+ *
+ * A row of head_dim channels is head_dim/2 bytes of codes and head_dim/32 bytes
+ * of scales: OCP microscaling with e2m1 elements (sign, and a magnitude of 0,
+ * 0.5, 1, 1.5, 2, 3, 4 or 6) and one E8M0 scale, a power of two, for each group
+ * of 32 neighbouring channels.  Channel 2i is the low half of byte i, channel
+ * 2i+1 the high half; scale byte b stands for 2^(b - 127), 255 for a group of
+ * NaN.  That is 4.25 bits a value.  A row carries its own scales, so that an
+ * eviction moves rows as they are.
+ *
+ * Codes (k, v) share one set of byte strides, scales (k_scale, v_scale) another:
+ * the codes of (seq s, layer l, KV head h, slot j) start at byte
+ *   s*stride_seq + l*stride_layer + h*stride_head + j*stride_slot,
+ * its scales at the same sum of the scale_ strides.  Codes: base and strides
+ * multiples of 16, stride_slot >= head_dim/2.  Scales: base and strides
+ * multiples of head_dim/32, scale_slot >= head_dim/32.  The four arrays do not
+ * overlap.  Calls that write a cache refuse sequences, layers or heads that
+ * share memory (stride 0).
+ */
+#define VD_MX4_MAX_CAPACITY (1 << 24)  /* slots per unit; an eviction takes VD_MAX_CAPACITY */
+
+typedef struct {
+    void *k, *v;              /* device; codes */
+    void *k_scale, *v_scale;  /* device; scales */
+    int32_t num_seqs, num_layers, num_kv_heads;  /* >= 1 */
+    int32_t num_q_heads;      /* multiple of num_kv_heads (GQA) */
+    int32_t head_dim;         /* 64, 128 or 256 */
+    int32_t capacity;         /* slots per unit, 1 .. VD_MX4_MAX_CAPACITY */
+    int64_t stride_seq, stride_layer, stride_head, stride_slot;  /* bytes, >= 0 */
+    int64_t scale_seq, scale_layer, scale_head, scale_slot;      /* bytes, >= 0 */
+} vd_mx4_cache;
+
+/*
+ * vd_append_mx4 -- new rows into the next slots of every unit, in 4 bits (Sec.
+ * 2.2, Eq. block_processing: the block is concatenated before the eviction).
+ *   n_old[s]   host; cached tokens of sequence s
+ *   rows[s]    host or NULL (max_rows each); its new rows, 0 .. max_rows, into
+ *              slots [n_old, n_old + rows) <= capacity
+ *   max_rows   >= 1; rows that the arrays hold for each sequence
+ *   dtype      vd_dtype of the rows
+ *   k_rows,    device; row r of (seq s, layer l, KV head h) starts at element
+ *   v_rows     s*strides[0] + l*strides[1] + h*strides[2] + r*strides[3],
+ *              head_dim contiguous elements, every row 16-byte aligned
+ *   k_strides, HOST arrays of four element strides, >= 0
+ *   v_strides
+ *   pos        device int32 [U][capacity] or NULL: slot n_old + r of every unit of
+ *              sequence s receives pos0[s] + r
+ *   pos0[s]    host, >= 0; NULL: n_old
+ * A group's scale is 2^e with the least e >= -127 for which the largest magnitude
+ * is below 7 * 2^e (at most 125, where 6 * 2^e is finite); a code is the
+ * nearest magnitude of value / 2^e, a tie to the even code, 6 at most, with the
+ * value's sign.  A group that holds an infinity or NaN becomes a group of NaN.
+ */
+vd_status vd_append_mx4(const vd_mx4_cache *cache, const int32_t *n_old, const int32_t *rows,
+                        int32_t max_rows, int32_t dtype, const void *k_rows, const int64_t *k_strides,
+                        const void *v_rows, const int64_t *v_strides, int32_t *pos,
+                        const int32_t *pos0, vd_stream stream);
+
+/*
+ * vd_read_mx4 -- the values that slots [first, first + rows) of every unit hold.
+ *   first[s]   host, >= 0
+ *   rows[s]    host or NULL (max_rows each); 0 .. max_rows, first + rows <= capacity
+ *   k_rows,    device, written; laid out as vd_append_mx4 reads them.  Rows at
+ *   v_rows     or above rows[s] are left as they were.
+ * Exact in fp32 and in bf16 (both also hold the smallest, 2^-128).
+ */
+vd_status vd_read_mx4(const vd_mx4_cache *cache, const int32_t *first, const int32_t *rows,
+                      int32_t max_rows, int32_t dtype, void *k_rows, const int64_t *k_strides,
+                      void *v_rows, const int64_t *v_strides, vd_stream stream);
+
+/*
+ * vd_attention_mx4 -- attention of the newest tokens of every sequence over its
+ * 4-bit cache (Sec. 2.1, Eq. attention): one row each in a decode step, a block
+ * in prompt processing (Sec. 2.2, Eq. block_processing).
+ *   dtype      vd_dtype of q and out
+ *   q          device; row i of (seq s, layer l, query head h) at element
+ *              s*q_strides[0] + l*q_strides[1] + h*q_strides[2] + i*q_strides[3],
+ *              head_dim contiguous elements, every row 16-byte aligned; query
+ *              head h uses KV head h / (num_q_heads / num_kv_heads)
+ *   max_rows   >= 1; query rows that q and out hold for each sequence
+ *   rows[s]    host or NULL (max_rows each); its query rows, 0 .. max_rows
+ *   n_valid[s] host; cached tokens, those of the query rows included: query row
+ *              i sees the slots j < n_valid - rows + 1 + i.  One that sees none gives 0.
+ *   scale      softmax scale, finite
+ *   out        device, laid out by out_strides; rows at or above rows[s] are
+ *              left as they were.  Must not overlap q or the cache.
+ *   workspace  device, 16-byte aligned, at least vd_attention_mx4_workspace_size()
+ *              bytes (may be NULL when that is 0); calls that share one must not overlap
+ * Logits, softmax and sums are fp32, products exact; a weight is rounded to bf16
+ * (2^-8 of it) for bf16 queries and to two bf16 parts (2^-16) for fp32 ones.  A cached
+ * row with a NaN group makes NaN of the outputs that see it, and of no other.
+ */
+vd_status vd_attention_mx4(const vd_mx4_cache *cache, int32_t dtype, const void *q,
+                           const int64_t *q_strides, int32_t max_rows, const int32_t *rows, float scale,
+                           const int32_t *n_valid, void *out, const int64_t *out_strides,
+                           void *workspace, size_t workspace_bytes, vd_stream stream);
+
+/* Bytes of workspace for a call whose longest sequence caches n tokens; it does
+ * not shrink with n, so n = capacity serves every call (0 for invalid arguments). */
+size_t vd_attention_mx4_workspace_size(const vd_mx4_cache *cache, int32_t dtype, int32_t max_rows,
+                                       int32_t n);
+
+/*
+ * vd_evict_step_mx4 -- the whole pass (mean, score, top-N, gather) of every unit
+ * of a 4-bit cache, in place and in one launch.  As vd_evict_step on the values
+ * that the cache holds, without a running sum: n_valid, budget, variant, pos,
+ * scores_out and keep_out are the same, so are the tie rule and the layout, and
+ * rows move with their scales.  Means and distances are fp64, rounded once to the
+ * fp32 scores that the selection ranks.  capacity <= VD_MAX_CAPACITY.
+ * A unit with a NaN group gives unspecified rankings.
+ */
+vd_status vd_evict_step_mx4(const vd_mx4_cache *cache, const int32_t *n_valid, const int32_t *budget,
+                            vd_variant variant, int32_t *pos, float *scores_out, uint8_t *keep_out,
+                            vd_stream stream);
+
+/*
+ * vd_qk_norm_rope -- the query and key rows that the attention takes: root mean
+ * square norm of each head's row and rotation by the token's position, in one pass.
+ *   y = x / sqrt(mean(x^2) + eps) * w      (w NULL: y = x)
+ *   for each pair i < rotary/2 of channels (a, b): (y_a, y_b) becomes
+ *   (y_a cos t - y_b sin t, y_b cos t + y_a sin t), t = pos * inv_freq[i],
+ *   with (a, b) = (i, i + rotary/2), or (2i, 2i + 1) where interleaved;
+ *   channels from `rotary` on are not rotated.
+ * Either side may be left out (its x and out NULL).  fp32 arithmetic, the angle in
+ * fp64, one rounding at the end.
+ */
+typedef struct {
+    const void *x;             /* device; row i of (seq, layer, head) by `strides` */
+    void *out;                 /* device; by `out_strides`; x itself, with its strides
+                                  and type, or memory that does not overlap it */
+    const void *weight;        /* device [num_layers][head_dim], 16-byte aligned, or NULL */
+    int64_t strides[4], out_strides[4];  /* seq, layer, head, row; elements, rows 16-byte aligned */
+    int32_t heads;             /* >= 1 */
+    int32_t out_dtype;         /* vd_dtype */
+} vd_rope_side;
+
+typedef struct {
+    vd_rope_side q, k;
+    const int32_t *pos;        /* device [num_seqs][rows] */
+    const float *inv_freq;     /* device [rotary/2], 16-byte aligned */
+    int32_t dtype;             /* vd_dtype of q and k */
+    int32_t weight_dtype;      /* vd_dtype of the weights */
+    int32_t num_seqs, num_layers, rows;  /* >= 1 */
+    int32_t head_dim;          /* 64, 128 or 256 */
+    int32_t rotary;            /* rotated channels: a multiple of 8, 8 .. head_dim */
+    int32_t interleaved;       /* 0 or 1 */
+    float eps;                 /* >= 0 */
+} vd_rope_args;
+
+vd_status vd_qk_norm_rope(const vd_rope_args *args, vd_stream stream);
+
 /* A static description of a status code. */
 const char *vd_status_string(vd_status status);
 

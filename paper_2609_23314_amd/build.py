@@ -43,12 +43,13 @@ def _build_one(out: str, defines, verbose: bool) -> str:
         objs = []
         steps = [
             [cc, f"--offload-arch={ARCH}", *COMMON, *defines, *DEVICE_FLAGS, "-c",
-             os.path.join(CSRC, "vd_kernels.hip"), "-o", os.path.join(tmp, "vd_kernels.o")],
+             os.path.join(CSRC, name + ".hip"), "-o", os.path.join(tmp, name + "_dev.o")]
+            for name in ("vd_kernels", "vd_mx4", "vd_rope")
         ] + [
             [cc, *COMMON, *defines, "-x", "c++", "-D__HIP_PLATFORM_AMD__",
              "-I", os.path.join(os.environ.get("ROCM_PATH", "/opt/rocm"), "include"),
              "-c", os.path.join(CSRC, name + ".cpp"), "-o", os.path.join(tmp, name + ".o")]
-            for name in ("vd_api", "vd_append")
+            for name in ("vd_api", "vd_append", "vd_mx4")
         ]
         for cmd in steps:
             if verbose:

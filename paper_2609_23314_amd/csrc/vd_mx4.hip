@@ -1,0 +1,760 @@
+// Kernels of a KV cache held in 4 bits: append, read, attention, eviction.
+//
+// A row of D channels is D / 2 bytes of e2m1 codes (channel 2i in the low half
+// of byte i) and D / 32 bytes of E8M0 scales, one power of two per 32 channels.
+// gfx950 converts both ways (v_cvt_scalef32_pk_*_fp4); code times scale is exact
+// in bf16, so that the matrix cores take a row's values without a rounding.
+#include <hip/hip_runtime.h>
+
+#include "vd.h"
+#include "vd_mx4.h"
+
+namespace vd {
+namespace {
+
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+
+template <class T>
+__device__ __forceinline__ uint32_t bits(T x) {
+    return __builtin_bit_cast(uint32_t, x);
+}
+__device__ __forceinline__ float as_float(uint32_t x) { return __builtin_bit_cast(float, x); }
+
+// The conversions' scale operand for an E8M0 byte: they read its exponent
+// alone, 0 as 2^-127 and 255 as NaN.
+__device__ __forceinline__ float scale_of(uint32_t byte) { return as_float(byte << 23); }
+
+template <int SEL>
+__device__ __forceinline__ bf16x2 decode2(uint32_t codes, float scale) {
+    return __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, SEL);
+}
+// Eight values of four bytes of codes.
+__device__ __forceinline__ bf16x8 decode8(uint32_t codes, float scale) {
+    const u32x4 r = {bits(decode2<0>(codes, scale)), bits(decode2<1>(codes, scale)), bits(decode2<2>(codes, scale)),
+                     bits(decode2<3>(codes, scale))};
+    return __builtin_bit_cast(bf16x8, r);
+}
+
+template <int CTRL>
+__device__ __forceinline__ uint32_t dpp(uint32_t x) {
+    return uint32_t(__builtin_amdgcn_update_dpp(0, int(x), CTRL, 0xF, 0xF, true));
+}
+constexpr int kXor1 = 0xB1, kXor2 = 0x4E;   // quad_perm
+
+// ---------------------------------------------------------------- append and read
+//
+// Eight channels a lane, the four lanes of a quad a group: the group's largest
+// magnitude is two exchanges in the quad away.  Bandwidth bounds both.
+
+// E8M0 byte of a group: the least exponent e >= -127 with max < 7 * 2^e, so
+// that the largest value rounds to at most 6 (code 7) and no value is cut by more
+// than its rounding; at most 125, where 6 * 2^e is still finite.  Anything not
+// finite makes the group NaN.
+__device__ __forceinline__ uint32_t group_scale(uint32_t max_bits) {
+    const int e = int(max_bits >> 23) - 2 + int((max_bits & 0x7FFFFFu) >= 0x600000u);
+    return max_bits >= 0x7F800000u ? 255u : uint32_t(min(max(e, 0), 252));
+}
+
+template <int DTYPE, int D>
+__global__ __launch_bounds__(kMxThreads) void append_kernel(const MxRowsParams p) {
+    constexpr int LANES = D / 8;
+    const uint32_t at = blockIdx.x * kMxThreads + threadIdx.x;
+    const int lane = at % LANES;
+    const uint32_t item = at / LANES;
+    const int row = int(item % uint32_t(p.max_rows)), unit = int(item / uint32_t(p.max_rows));
+    const bool is_v = blockIdx.y & 1;
+    const int s = blockIdx.y >> 1;
+    if (unit >= p.c.layers * p.c.heads || row >= p.rows[s]) return;   // (a row's lanes leave together)
+    const int layer = unit / p.c.heads, head = unit % p.c.heads;
+    const char *src = (is_v ? p.v + s * p.vs[0] + layer * p.vs[1] + head * p.vs[2] + row * p.vs[3]
+                            : p.k + s * p.ks[0] + layer * p.ks[1] + head * p.ks[2] + row * p.ks[3]);
+    uint32_t x[8];
+    if (DTYPE == VD_DTYPE_F32) {
+        const u32x4 u = reinterpret_cast<const u32x4 *>(src)[2 * lane], w = reinterpret_cast<const u32x4 *>(src)[2 * lane + 1];
+        for (int i = 0; i < 4; ++i) x[i] = u[i], x[4 + i] = w[i];
+    } else {
+        const u32x4 u = reinterpret_cast<const u32x4 *>(src)[lane];
+        for (int i = 0; i < 4; ++i) x[2 * i] = u[i] << 16, x[2 * i + 1] = u[i] & 0xFFFF0000u;
+    }
+    uint32_t top = 0;
+    for (int i = 0; i < 8; ++i) top = max(top, x[i] & 0x7FFFFFFFu);
+    top = max(top, dpp<kXor1>(top));
+    top = max(top, dpp<kXor2>(top));
+    const uint32_t byte = group_scale(top);
+    const float scale = scale_of(byte);
+    uint32_t codes = 0;
+    codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, as_float(x[0]), as_float(x[1]), scale, 0);
+    codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, as_float(x[2]), as_float(x[3]), scale, 1);
+    codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, as_float(x[4]), as_float(x[5]), scale, 2);
+    codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, as_float(x[6]), as_float(x[7]), scale, 3);
+    if (byte == 255u) codes = 0;
+    const int slot = p.first[s] + row;
+    char *dst = (is_v ? p.c.v : p.c.k) + s * p.c.seq + layer * p.c.layer + head * p.c.head + uint32_t(slot) * p.c.slot;
+    char *sdst = (is_v ? p.c.vs : p.c.ks) + s * p.c.sseq + layer * p.c.slayer + head * p.c.shead + uint32_t(slot) * p.c.sslot;
+    reinterpret_cast<uint32_t *>(dst)[lane] = codes;
+    if ((lane & 3) == 0) sdst[lane >> 2] = char(byte);
+    if (p.pos && !is_v && lane == 0)
+        p.pos[(int64_t(s) * p.c.layers * p.c.heads + unit) * p.capacity + slot] = p.pos0[s] + row;
+}
+
+template <int DTYPE, int D>
+__global__ __launch_bounds__(kMxThreads) void read_kernel(const MxRowsParams p) {
+    constexpr int LANES = D / 8;
+    const uint32_t at = blockIdx.x * kMxThreads + threadIdx.x;
+    const int lane = at % LANES;
+    const uint32_t item = at / LANES;
+    const int row = int(item % uint32_t(p.max_rows)), unit = int(item / uint32_t(p.max_rows));
+    const bool is_v = blockIdx.y & 1;
+    const int s = blockIdx.y >> 1;
+    if (unit >= p.c.layers * p.c.heads || row >= p.rows[s]) return;
+    const int layer = unit / p.c.heads, head = unit % p.c.heads;
+    const uint32_t slot = uint32_t(p.first[s] + row);
+    const char *src = (is_v ? p.c.v : p.c.k) + s * p.c.seq + layer * p.c.layer + head * p.c.head + slot * p.c.slot;
+    const char *ssrc = (is_v ? p.c.vs : p.c.ks) + s * p.c.sseq + layer * p.c.slayer + head * p.c.shead + slot * p.c.sslot;
+    const uint32_t codes = reinterpret_cast<const uint32_t *>(src)[lane];
+    const float scale = scale_of(uint8_t(ssrc[lane >> 2]));
+    char *dst = (is_v ? p.v + s * p.vs[0] + layer * p.vs[1] + head * p.vs[2] + row * p.vs[3]
+                      : p.k + s * p.ks[0] + layer * p.ks[1] + head * p.ks[2] + row * p.ks[3]);
+    if (DTYPE == VD_DTYPE_F32) {
+        const f32x2 a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, scale, 0);
+        const f32x2 b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, scale, 1);
+        const f32x2 c = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, scale, 2);
+        const f32x2 d = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, scale, 3);
+        reinterpret_cast<f32x4 *>(dst)[2 * lane] = f32x4{a[0], a[1], b[0], b[1]};
+        reinterpret_cast<f32x4 *>(dst)[2 * lane + 1] = f32x4{c[0], c[1], d[0], d[1]};
+    } else {
+        reinterpret_cast<bf16x8 *>(dst)[lane] = decode8(codes, scale);
+    }
+}
+
+// ---------------------------------------------------------------- attention
+//
+// out_i = sum_j w_ij v_j, w_ij = exp(scale q_i.k_j - m_i) / sum, over the slots
+// j < n - rows + 1 + i that query row i sees.  The G query heads of a KV head
+// share its rows, so a tile's 16 query rows are m = i * G + g.
+//
+// A wave takes 32 cache rows at a time.  A lane reads a quarter of a row's codes
+// (16 bytes at D = 128: one whole group, one scale) and converts them into the
+// left operand of v_mfma_f32_16x16x32_bf16, whose sum over channels may take them
+// in any order: here the quarter's eight by eight.  Its output has a lane hold one
+// query's logits for 4 rows of 16, which is, for 32 rows, just the right operand of
+// the product with V^T: weights never leave their lane.  V's rows are converted
+// the same way, and turned in LDS: written by row, read by ds_read_b64_tr_b16.
+//
+// fp32 queries are three bf16 parts (exact), their weights two (2^-16 of a weight);
+// bf16 queries take one part each (a weight's rounding is 2^-8 of it, as the
+// output's; the sum of the weights is that of the rounded ones, so that a row with
+// one weight is exact).  Sums, logits and the softmax are fp32.
+//
+// A row with a NaN group, in K or in V, makes NaN of the outputs that see it and
+// only those: its K scale becomes NaN, and V's stays finite.
+
+template <int D>
+struct Quarter {   // a lane's part of a row: D / 4 channels
+    static constexpr int WORDS = D / 32;
+    uint32_t w[WORDS];
+};
+template <int D>
+__device__ __forceinline__ Quarter<D> load_quarter(const char *row, int kq) {
+    Quarter<D> r;
+    if (D == 64) {
+        const u32x2 x = reinterpret_cast<const u32x2 *>(row)[kq];
+        r.w[0] = x[0], r.w[1] = x[1];
+    } else {
+        for (int i = 0; i < D / 128; ++i) {
+            const u32x4 x = reinterpret_cast<const u32x4 *>(row)[kq * (D / 128) + i];
+            for (int e = 0; e < 4; ++e) r.w[(4 * i + e) % (D / 32)] = x[e];
+        }
+    }
+    return r;
+}
+// All scales of a row.
+template <int D>
+struct Scales {
+    static constexpr int WORDS = D == 256 ? 2 : 1;
+    uint32_t w[WORDS];
+    __device__ __forceinline__ uint32_t byte(int group) const {
+        const uint32_t x = WORDS == 2 && group >= 4 ? w[WORDS - 1] : w[0];
+        return (x >> (8 * (group & 3))) & 255u;
+    }
+    __device__ __forceinline__ bool has_nan() const {
+        bool nan = false;
+        for (int i = 0; i < WORDS; ++i) nan |= ((~w[i] - 0x01010101u) & w[i] & 0x80808080u) != 0;   // a zero byte of ~w
+        return nan;
+    }
+};
+template <int D>
+__device__ __forceinline__ Scales<D> load_scales(const char *row) {
+    Scales<D> r;
+    if (D == 64) {
+        r.w[0] = *reinterpret_cast<const uint16_t *>(row);
+    } else if (D == 128) {
+        r.w[0] = *reinterpret_cast<const uint32_t *>(row);
+    } else {
+        const u32x2 x = *reinterpret_cast<const u32x2 *>(row);
+        r.w[0] = x[0], r.w[Scales<D>::WORDS - 1] = x[1];
+    }
+    return r;
+}
+
+// Bytes of one wave's V tile: 32 rows of bf16, 32 bytes apart from a multiple
+// of the banks, so that neither the rows' writes nor the turned reads collide.
+template <int D>
+constexpr int kVStride = D * 2 + 32;
+
+template <int D>
+constexpr int attn_lds() {
+    const int tiles = 4 * 32 * kVStride<D>, merge = 4 * kMxTile * (D + 4) * 4 + 4 * kMxTile * 2 * 4;
+    return tiles > merge ? tiles : merge;
+}
+
+struct AttnUnit {   // what a workgroup works on
+    int n, rows, queries;        // cached rows, query rows, query rows times heads
+    int begin, end;              // its rows of the cache
+};
+
+template <int DTYPE, int D>
+__global__ __launch_bounds__(kMxThreads) void attn_kernel(const MxAttnParams p) {
+    constexpr int FRAGS = D / 32;                                // products over the channels of one logit tile
+    constexpr int QP = DTYPE == VD_DTYPE_F32 ? 3 : 1;            // parts of a query
+    constexpr int PP = DTYPE == VD_DTYPE_F32 ? 2 : 1;            // parts of a weight
+    constexpr int CT = D / 16;                                   // channel tiles of the output
+    __shared__ __attribute__((aligned(16))) char lds[attn_lds<D>()];
+    const int split = blockIdx.x / p.tiles, tile = blockIdx.x % p.tiles;
+    const int head = blockIdx.y, s = blockIdx.z / p.c.layers, layer = blockIdx.z % p.c.layers;
+    const int n = p.n[s], rows = p.rows[s], G = p.group;
+    const int queries = rows * G, m0 = tile * kMxTile;
+    if (m0 >= queries) return;
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, c = lane & 15, kq = lane >> 4;
+    // the cache rows that any query of the tile sees, and this split's share of them
+    const int seen = max(0, n - rows + 1 + min(m0 + kMxTile - 1, queries - 1) / G);
+    const int share = ((seen + p.splits - 1) / p.splits + 127) & ~127;
+    const int begin = min(split * share, seen), end = min(begin + share, seen);
+    const int all_see = n - rows + 1 + m0 / G;                   // rows below this need no mask
+    const int m = m0 + c, i = min(m, queries - 1) / G, g = min(m, queries - 1) - i * G;
+    const int limit = n - rows + 1 + i;
+
+    // queries: the right operand, channels kq * D / 4 + 8 f + e of query c
+    bf16x8 q[QP][FRAGS];
+    {
+        const char *src = p.q + s * p.qs[0] + layer * p.qs[1] + (head * G + g) * p.qs[2] + i * p.qs[3];
+#pragma unroll
+        for (int f = 0; f < FRAGS; ++f) {
+            const int ch = kq * (D / 4) + 8 * f;
+            if (DTYPE == VD_DTYPE_BF16) {
+                q[0][f] = *reinterpret_cast<const bf16x8 *>(src + ch * 2);
+            } else {
+                const f32x4 a = *reinterpret_cast<const f32x4 *>(src + ch * 4), b = *reinterpret_cast<const f32x4 *>(src + ch * 4 + 16);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    float x = e < 4 ? a[e & 3] : b[e & 3];
+#pragma unroll
+                    for (int part = 0; part < QP; ++part) {
+                        q[part][f][e] = __bf16(x);
+                        x -= float(q[part][f][e]);
+                    }
+                }
+            }
+        }
+    }
+
+    const char *kb = p.c.k + s * p.c.seq + layer * p.c.layer + head * p.c.head;
+    const char *vb = p.c.v + s * p.c.seq + layer * p.c.layer + head * p.c.head;
+    const char *ksb = p.c.ks + s * p.c.sseq + layer * p.c.slayer + head * p.c.shead;
+    const char *vsb = p.c.vs + s * p.c.sseq + layer * p.c.slayer + head * p.c.shead;
+    char *tile_lds = lds + wave * 32 * kVStride<D>;
+
+    f32x4 acc[CT + 1];   // the last: sum of the weights (a column of ones beside V)
+#pragma unroll
+    for (int t = 0; t <= CT; ++t) acc[t] = f32x4{0, 0, 0, 0};
+    const uint32_t one2 = 0x3F803F80u;
+    const bf16x8 ones = __builtin_bit_cast(bf16x8, (u32x4{one2, one2, one2, one2}));
+    float top = -INFINITY, sub = 0.0f;   // the maximum that the weights are relative to
+
+    for (int j0 = begin + 32 * wave; j0 < end; j0 += 128) {
+        Quarter<D> kc[2], vc[2];
+        Scales<D> ks[2], vs[2];
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {   // rows behind the end: the last row again, hidden below
+            const uint32_t row = uint32_t(min(j0 + 16 * t + c, end - 1));
+            kc[t] = load_quarter<D>(kb + row * p.c.slot, kq);
+            ks[t] = load_scales<D>(ksb + row * p.c.sslot);
+            vc[t] = load_quarter<D>(vb + row * p.c.slot, kq);
+            vs[t] = load_scales<D>(vsb + row * p.c.sslot);
+        }
+        f32x4 z[2];
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            const bool nan = ks[t].has_nan() || vs[t].has_nan();
+            z[t] = f32x4{0, 0, 0, 0};
+#pragma unroll
+            for (int f = 0; f < FRAGS; ++f) {
+                const int group = (kq * (D / 4) + 8 * f) / kMxGroup;
+                const float scale = scale_of(nan ? 255u : ks[t].byte(group));
+                const bf16x8 a = decode8(kc[t].w[f], scale);
+#pragma unroll
+                for (int part = QP - 1; part >= 0; --part)
+                    z[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, q[part][f], z[t], 0, 0, 0);
+                const uint32_t vbyte = vs[t].byte(group);
+                const float vscale = scale_of(vbyte == 255u ? 0u : vbyte);
+                *reinterpret_cast<bf16x8 *>(tile_lds + (16 * t + c) * kVStride<D> + (kq * (D / 4) + 8 * f) * 2) = decode8(vc[t].w[f], vscale);
+            }
+        }
+        // lane: query c, rows j0 + 16 t + 4 kq + r
+        float best = -INFINITY;
+        const bool masked = j0 + 32 > min(all_see, end);
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                float x = z[t][r] * p.qscale;
+                if (masked) x = j0 + 16 * t + 4 * kq + r < min(limit, end) ? x : -INFINITY;
+                z[t][r] = x;
+                best = fmaxf(best, x);
+            }
+        // The weights are relative to a maximum that is raised only when a logit
+        // passes it by 8 (log2 units): they stay below 2^8, and mostly no sum is rescaled.
+        if (__builtin_amdgcn_ballot_w64(best > top + 8.0f)) {
+            best = fmaxf(best, __shfl_xor(best, 16));
+            best = fmaxf(best, __shfl_xor(best, 32));
+            const float next = fmaxf(top, best);
+            const float down = __builtin_amdgcn_exp2f(top - (next == -INFINITY ? 0.0f : next));
+            top = next;
+            sub = next == -INFINITY ? 0.0f : next;
+#pragma unroll
+            for (int t = 0; t <= CT; ++t)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) acc[t][r] *= down;
+        }
+        bf16x8 w[PP];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            float x = __builtin_amdgcn_exp2f(z[e >> 2][e & 3] - sub);
+#pragma unroll
+            for (int part = 0; part < PP; ++part) {
+                w[part][e] = __bf16(x);
+                x -= float(w[part][e]);
+            }
+        }
+#pragma unroll
+        for (int ct = 0; ct < CT; ++ct) {
+            typedef __attribute__((address_space(3))) s16x4 *lds4;
+            const char *at = tile_lds + (4 * kq + (c >> 2)) * kVStride<D> + ct * 32 + (c & 3) * 8;
+            const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(at));
+            const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(at + 16 * kVStride<D>));
+            const bf16x8 a = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+#pragma unroll
+            for (int part = PP - 1; part >= 0; --part)
+                acc[ct] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, w[part], acc[ct], 0, 0, 0);
+        }
+#pragma unroll
+        for (int part = PP - 1; part >= 0; --part)
+            acc[CT] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, w[part], acc[CT], 0, 0, 0);
+    }
+
+    // the four waves' sums
+    __syncthreads();
+    float *part = reinterpret_cast<float *>(lds);                         // [wave][query][D + 4]
+    float *ml = part + 4 * kMxTile * (D + 4);                             // [wave][query][2]
+#pragma unroll
+    for (int ct = 0; ct < CT; ++ct)
+        *reinterpret_cast<f32x4 *>(part + (wave * kMxTile + c) * (D + 4) + 16 * ct + 4 * kq) = acc[ct];
+    if (kq == 0) {
+        ml[(wave * kMxTile + c) * 2] = top;
+        ml[(wave * kMxTile + c) * 2 + 1] = acc[CT][0];
+    }
+    __syncthreads();
+    const int count = min(kMxTile, queries - m0);
+    const int64_t unit = (int64_t(s) * p.c.layers + layer) * p.c.heads + head;
+    const int64_t all = int64_t(p.max_rows) * G;
+    for (int at = threadIdx.x; at < count * (D / 4); at += kMxThreads) {
+        const int query = at / (D / 4), ch = at % (D / 4) * 4;
+        float tops[4], high = -INFINITY, sum = 0.0f;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) high = fmaxf(high, tops[w] = ml[(w * kMxTile + query) * 2]);
+        f32x4 o = {0, 0, 0, 0};
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            // (a wave without a finite logit has no weights, or only NaN ones)
+            const float f = tops[w] == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(tops[w] - high);
+            const f32x4 x = *reinterpret_cast<const f32x4 *>(part + (w * kMxTile + query) * (D + 4) + ch);
+            sum = fmaf(ml[(w * kMxTile + query) * 2 + 1], f, sum);
+            for (int e = 0; e < 4; ++e) o[e] = fmaf(x[e], f, o[e]);
+        }
+        if (p.splits > 1) {
+            const int64_t to = (unit * p.splits + split) * all + m0 + query;
+            *reinterpret_cast<f32x4 *>(p.ws_acc + to * D + ch) = o;
+            if (ch == 0) p.ws_ml[to * 2] = high, p.ws_ml[to * 2 + 1] = sum;
+            continue;
+        }
+        const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;     // no row seen: 0
+        const int qi = (m0 + query) / G, qg = (m0 + query) - qi * G;
+        char *dst = p.out + s * p.os[0] + layer * p.os[1] + (head * G + qg) * p.os[2] + qi * p.os[3];
+        if (DTYPE == VD_DTYPE_F32) {
+            *reinterpret_cast<f32x4 *>(dst + ch * 4) = o * inv;
+        } else {
+            bf16x4 b;
+            for (int e = 0; e < 4; ++e) b[e] = __bf16(o[e] * inv);
+            *reinterpret_cast<bf16x4 *>(dst + ch * 2) = b;
+        }
+    }
+}
+
+// Joins the splits of a query row: a wave a row, a lane D / 64 channels.
+template <int DTYPE, int D>
+__global__ __launch_bounds__(kMxThreads) void attn_join_kernel(const MxAttnParams p) {
+    constexpr int CH = D / 64;
+    const int G = p.group, lane = threadIdx.x & 63;
+    const int head = blockIdx.y, s = blockIdx.z / p.c.layers, layer = blockIdx.z % p.c.layers;
+    const int query = blockIdx.x * (kMxThreads / 64) + (threadIdx.x >> 6);
+    if (query >= p.rows[s] * G) return;
+    const int64_t unit = (int64_t(s) * p.c.layers + layer) * p.c.heads + head;
+    const int64_t all = int64_t(p.max_rows) * G, first = unit * p.splits * all + query;
+    const bool mine = lane < p.splits;
+    const float top = mine ? p.ws_ml[(first + lane * all) * 2] : -INFINITY;
+    const float sum = mine ? p.ws_ml[(first + lane * all) * 2 + 1] : 0.0f;
+    float high = top;
+    for (int d = 1; d < 64; d *= 2) high = fmaxf(high, __shfl_xor(high, d));
+    const float f = top == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(top - high);
+    float total = sum * f;
+    for (int d = 1; d < 64; d *= 2) total += __shfl_xor(total, d);
+    float o[CH] = {};
+    for (int split = 0; split < p.splits; ++split) {
+        const float w = __shfl(f, split);
+        const float *x = p.ws_acc + (first + split * all) * D + lane * CH;
+        for (int e = 0; e < CH; ++e) o[e] = fmaf(x[e], w, o[e]);
+    }
+    const float inv = total == 0.0f ? 0.0f : 1.0f / total;
+    const int qi = query / G, qg = query - qi * G;
+    char *dst = p.out + s * p.os[0] + layer * p.os[1] + (head * G + qg) * p.os[2] + qi * p.os[3];
+    for (int e = 0; e < CH; ++e) {
+        if (DTYPE == VD_DTYPE_F32)
+            reinterpret_cast<float *>(dst)[lane * CH + e] = o[e] * inv;
+        else
+            reinterpret_cast<__bf16 *>(dst)[lane * CH + e] = __bf16(o[e] * inv);
+    }
+}
+
+// ---------------------------------------------------------------- eviction
+//
+// One workgroup a unit: the column sums of its scored rows, their distances from
+// the mean, the N highest, the gather.  Values are exact, sums and distances fp64:
+// the fp32 scores, which the selection ranks, are correctly rounded but for a
+// last-bit tie, whatever the order of the sums.
+
+constexpr int kEvictWaves = kMxEvictThreads / 64;
+
+struct EvictHead {
+    uint32_t hist[256];
+    uint32_t word[8];               // broadcast
+    uint32_t count[2][kEvictWaves];
+    unsigned long long low[kEvictWaves];
+    double mean[256];
+    double len[1];
+};
+
+__device__ __forceinline__ double shfl_xor_double(double x, int d) {
+    const unsigned long long b = __builtin_bit_cast(unsigned long long, x);
+    const uint32_t lo = __shfl_xor(uint32_t(b), d), hi = __shfl_xor(uint32_t(b >> 32), d);
+    return __builtin_bit_cast(double, (unsigned long long)(hi) << 32 | lo);
+}
+
+// A larger key ranks higher; KeyNorm keeps the smallest norms.
+__device__ __forceinline__ uint32_t rank_key(float score, bool smallest) {
+    uint32_t b = bits(score == 0.0f ? 0.0f : score);
+    b = b & 0x80000000u ? ~b : b | 0x80000000u;
+    return smallest ? ~b : b;
+}
+
+template <int D>
+__global__ __launch_bounds__(kMxEvictThreads) void evict_kernel(const MxEvictParams p) {
+    constexpr int LANES = D / 32;                         // lanes of a row: a group each
+    constexpr int ROWS = kMxEvictThreads / LANES;         // rows that the workgroup takes at a time
+    extern __shared__ __attribute__((aligned(16))) char dyn[];
+    __shared__ EvictHead sh;
+    uint32_t *keys = reinterpret_cast<uint32_t *>(dyn);
+    uint16_t *holes = reinterpret_cast<uint16_t *>(dyn + p.off_lists), *movers = holes + p.list_cap;
+    double *partial = reinterpret_cast<double *>(dyn);    // [wave][D], before the keys
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int head = blockIdx.x, layer = blockIdx.y, s = blockIdx.z;
+    const int n = p.n[s], N = p.budget[s];
+    if (n == 0) return;
+    const int64_t unit = (int64_t(s) * p.c.layers + layer) * p.c.heads + head;
+    const int64_t code_at = s * p.c.seq + layer * p.c.layer + head * p.c.head;
+    const int64_t scale_at = s * p.c.sseq + layer * p.c.slayer + head * p.c.shead;
+    const bool key_side = p.variant >= VD_SCORE_KEY_L2;
+    const int form = p.variant - (key_side ? VD_SCORE_KEY_L2 : 0);   // L2, Dir, Norm
+    const bool smallest = p.variant == VD_SCORE_KEY_NORM;
+    float *scores = p.scores ? p.scores + unit * p.capacity : nullptr;
+    uint8_t *keep = p.keep ? p.keep + unit * p.capacity : nullptr;
+    if (n <= N && !scores) {
+        if (keep)
+            for (int j = tid; j < n; j += kMxEvictThreads) keep[j] = 1;
+        return;
+    }
+    const char *xb = (key_side ? p.c.k : p.c.v) + code_at, *sb = (key_side ? p.c.ks : p.c.vs) + scale_at;
+    const int g = tid % LANES, r0 = tid / LANES;
+
+    double mean[32];
+#pragma unroll
+    for (int i = 0; i < 32; ++i) mean[i] = 0.0;
+    if (form != VD_SCORE_NORM) {
+        for (int j = r0; j < n; j += ROWS) {
+            const u32x4 x = reinterpret_cast<const u32x4 *>(xb + uint32_t(j) * p.c.slot)[g];
+            const float scale = scale_of(uint8_t(sb[uint32_t(j) * p.c.sslot + g]));
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+                const f32x2 a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(x[w], scale, 0);
+                const f32x2 b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(x[w], scale, 1);
+                const f32x2 c = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(x[w], scale, 2);
+                const f32x2 d = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(x[w], scale, 3);
+                mean[8 * w + 0] += double(a[0]), mean[8 * w + 1] += double(a[1]);
+                mean[8 * w + 2] += double(b[0]), mean[8 * w + 3] += double(b[1]);
+                mean[8 * w + 4] += double(c[0]), mean[8 * w + 5] += double(c[1]);
+                mean[8 * w + 6] += double(d[0]), mean[8 * w + 7] += double(d[1]);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < 32; ++i) {
+#pragma unroll
+            for (int d = LANES; d < 64; d *= 2) mean[i] += shfl_xor_double(mean[i], d);
+            if (lane < LANES) partial[wave * D + lane * 32 + i] = mean[i];
+        }
+        __syncthreads();
+        if (tid < D) {
+            double t = 0.0;
+            for (int w = 0; w < kEvictWaves; ++w) t += partial[w * D + tid];
+            sh.mean[tid] = t / double(n);
+        }
+        __syncthreads();
+        if (form == VD_SCORE_DIR && wave == 0) {
+            double t = 0.0;
+            for (int c = lane; c < D; c += 64) t = fma(sh.mean[c], sh.mean[c], t);
+            for (int d = 1; d < 64; d *= 2) t += shfl_xor_double(t, d);
+            if (lane == 0) sh.len[0] = sqrt(t);
+        }
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < 32; ++i) mean[i] = sh.mean[g * 32 + i];
+    }
+    const double length = form == VD_SCORE_DIR ? sh.len[0] : 0.0;
+
+    for (int j = r0; j < n; j += ROWS) {
+        const u32x4 x = reinterpret_cast<const u32x4 *>(xb + uint32_t(j) * p.c.slot)[g];
+        const float scale = scale_of(uint8_t(sb[uint32_t(j) * p.c.sslot + g]));
+        double sq = 0.0, dot = 0.0;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            const f32x2 y[4] = {__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(x[w], scale, 0), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(x[w], scale, 1),
+                                __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(x[w], scale, 2), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(x[w], scale, 3)};
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const double v = double(y[e >> 1][e & 1]), m = mean[8 * w + e];
+                if (form == VD_SCORE_DIR) {
+                    sq = fma(v, v, sq);
+                    dot = fma(v, m, dot);
+                } else {
+                    sq = fma(v - m, v - m, sq);   // (Norm: m is 0)
+                }
+            }
+        }
+#pragma unroll
+        for (int d = 1; d < LANES; d *= 2) sq += shfl_xor_double(sq, d), dot += shfl_xor_double(dot, d);
+        if (g == 0) {
+            double score = sqrt(sq);
+            if (form == VD_SCORE_DIR) {
+                const double both = score * length;
+                score = both > 0.0 ? 1.0 - dot / both : both == 0.0 ? 1.0 : both;
+            }
+            const float out = float(score);
+            if (scores) scores[j] = out;
+            if (n > N) keys[j] = rank_key(out, smallest);
+        }
+    }
+    if (n <= N) {
+        if (keep)
+            for (int j = tid; j < n; j += kMxEvictThreads) keep[j] = 1;
+        return;
+    }
+    __syncthreads();
+
+    int moved;   // rows to move: movers[k] onto holes[k]
+    if (n == N + 1) {
+        // the lowest key goes, the highest slot among equal ones
+        unsigned long long low = ~0ull;
+        for (int j = tid; j < n; j += kMxEvictThreads) {
+            const unsigned long long at = (unsigned long long)(keys[j]) << 32 | uint32_t(~j);
+            low = at < low ? at : low;
+        }
+        for (int d = 1; d < 64; d *= 2) {
+            const uint32_t a = __shfl_xor(uint32_t(low), d), b = __shfl_xor(uint32_t(low >> 32), d);
+            const unsigned long long o = (unsigned long long)(b) << 32 | a;
+            low = o < low ? o : low;
+        }
+        if (lane == 0) sh.low[wave] = low;
+        __syncthreads();
+        for (int w = 0; w < kEvictWaves; ++w) low = sh.low[w] < low ? sh.low[w] : low;
+        const int gone = int(~uint32_t(low));
+        if (keep)
+            for (int j = tid; j < n; j += kMxEvictThreads) keep[j] = j != gone;
+        if (tid == 0) holes[0] = uint16_t(gone), movers[0] = uint16_t(N);
+        moved = gone < N;
+        __syncthreads();
+    } else {
+        // the N-th highest key by its bytes, highest first
+        uint32_t prefix = 0;
+        int want = N;   // rows still to find among those that share the prefix
+        for (int shift = 24; shift >= 0; shift -= 8) {
+            if (tid < 256) sh.hist[tid] = 0;
+            __syncthreads();
+            for (int j = tid; j < n; j += kMxEvictThreads) {
+                const uint32_t key = keys[j];
+                if (shift == 24 || (key >> (shift + 8)) == (prefix >> (shift + 8))) atomicAdd(&sh.hist[(key >> shift) & 255u], 1u);
+            }
+            __syncthreads();
+            if (wave == 0) {   // lane: bins 255 - 4 lane downwards
+                uint32_t c[4], sum = 0;
+                for (int i = 0; i < 4; ++i) sum += c[i] = sh.hist[255 - 4 * lane - i];
+                uint32_t upto = sum;
+                for (int d = 1; d < 64; d *= 2) {
+                    const uint32_t o = __shfl_up(upto, d);
+                    if (lane >= d) upto += o;
+                }
+                uint32_t before = upto - sum;
+                for (int i = 0; i < 4; ++i) {
+                    if (before < uint32_t(want) && before + c[i] >= uint32_t(want)) {
+                        sh.word[0] = uint32_t(255 - 4 * lane - i);
+                        sh.word[1] = before;
+                    }
+                    before += c[i];
+                }
+            }
+            __syncthreads();
+            prefix |= sh.word[0] << shift;
+            want -= int(sh.word[1]);
+        }
+        // keys above `prefix` stay, and of those equal to it the first `want`
+        int ties = 0, nh = 0, nm = 0;   // so far
+        const unsigned long long below = (1ull << lane) - 1;
+        for (int base = 0; base < n; base += kMxEvictThreads) {
+            const int j = base + tid;
+            const uint32_t key = j < n ? keys[j] : 0u;
+            const bool tie = j < n && key == prefix;
+            const unsigned long long tb = __builtin_amdgcn_ballot_w64(tie);
+            if (lane == 0) sh.count[0][wave] = __popcll(tb);
+            __syncthreads();
+            int tie_rank = ties + __popcll(tb & below);
+            for (int w = 0; w < kEvictWaves; ++w) {
+                tie_rank += w < wave ? int(sh.count[0][w]) : 0;
+                ties += int(sh.count[0][w]);
+            }
+            __syncthreads();
+            const bool kept = j < n && (key > prefix || (tie && tie_rank < want));
+            if (keep && j < n) keep[j] = kept;
+            const bool hole = j < min(N, n) && !kept, mover = kept && j >= N;
+            const unsigned long long hb = __builtin_amdgcn_ballot_w64(hole), mb = __builtin_amdgcn_ballot_w64(mover);
+            if (lane == 0) sh.count[0][wave] = __popcll(hb), sh.count[1][wave] = __popcll(mb);
+            __syncthreads();
+            int hr = nh + __popcll(hb & below), mr = nm + __popcll(mb & below);
+            for (int w = 0; w < kEvictWaves; ++w) {
+                hr += w < wave ? int(sh.count[0][w]) : 0;
+                mr += w < wave ? int(sh.count[1][w]) : 0;
+                nh += int(sh.count[0][w]);
+                nm += int(sh.count[1][w]);
+            }
+            if (hole && hr < p.list_cap) holes[hr] = uint16_t(j);
+            if (mover && mr < p.list_cap) movers[mr] = uint16_t(j);
+            __syncthreads();
+        }
+        moved = min(min(nh, nm), p.list_cap);
+    }
+
+    // codes in 16-byte words (K's, then V's), scales in one word of D / 32 bytes
+    constexpr int WORDS = D / 32;
+    char *kb = p.c.k + code_at, *vb = p.c.v + code_at, *ksb = p.c.ks + scale_at, *vsb = p.c.vs + scale_at;
+    for (int at = tid; at < moved * 2 * WORDS; at += kMxEvictThreads) {
+        const int i = at / (2 * WORDS), w = at % (2 * WORDS);
+        char *b = w < WORDS ? kb : vb;
+        const uint32_t to = holes[i], from = movers[i];
+        reinterpret_cast<u32x4 *>(b + to * p.c.slot)[w % WORDS] = reinterpret_cast<const u32x4 *>(b + from * p.c.slot)[w % WORDS];
+    }
+    for (int at = tid; at < moved * 2; at += kMxEvictThreads) {
+        char *b = at & 1 ? vsb : ksb;
+        const uint32_t to = holes[at >> 1], from = movers[at >> 1];
+        if (D == 64)
+            *reinterpret_cast<uint16_t *>(b + to * p.c.sslot) = *reinterpret_cast<const uint16_t *>(b + from * p.c.sslot);
+        else if (D == 128)
+            *reinterpret_cast<uint32_t *>(b + to * p.c.sslot) = *reinterpret_cast<const uint32_t *>(b + from * p.c.sslot);
+        else
+            *reinterpret_cast<u32x2 *>(b + to * p.c.sslot) = *reinterpret_cast<const u32x2 *>(b + from * p.c.sslot);
+    }
+    if (p.pos) {
+        int32_t *pos = p.pos + unit * p.capacity;
+        for (int i = tid; i < moved; i += kMxEvictThreads) pos[holes[i]] = pos[movers[i]];
+    }
+}
+
+}  // namespace
+
+// ---------------------------------------------------------------- launches
+
+namespace {
+
+template <class P, class F>
+hipError_t launch_rows(const P &p, int seqs, int head_dim, F kernel, hipStream_t stream) {
+    const int64_t threads = int64_t(p.c.layers) * p.c.heads * p.max_rows * (head_dim / 8);
+    const dim3 grid(uint32_t((threads + kMxThreads - 1) / kMxThreads), uint32_t(2 * seqs));
+    return launch_with<P>(kernel, grid, kMxThreads, 0, stream, p);
+}
+
+template <int DTYPE, int D>
+hipError_t launch_attn(const MxAttnParams &p, int seqs, hipStream_t stream) {
+    const dim3 grid(uint32_t(p.splits) * p.tiles, p.c.heads, seqs * p.c.layers);
+    const hipError_t e = launch_with(attn_kernel<DTYPE, D>, grid, kMxThreads, 0, stream, p);
+    if (e != hipSuccess || p.splits == 1) return e;
+    const uint32_t per = kMxThreads / 64;
+    const dim3 join((uint32_t(p.max_rows) * p.group + per - 1) / per, p.c.heads, seqs * p.c.layers);
+    return launch_with(attn_join_kernel<DTYPE, D>, join, kMxThreads, 0, stream, p);
+}
+
+template <int D>
+hipError_t launch_evict(const MxEvictParams &p, int seqs, size_t lds, hipStream_t stream) {
+    return launch_with(evict_kernel<D>, dim3(p.c.heads, p.c.layers, seqs), kMxEvictThreads, lds, stream, p);
+}
+
+}  // namespace
+
+hipError_t launch_mx_append(const MxRowsParams &p, int seqs, int dtype, int D, hipStream_t stream) {
+    const bool b = dtype == VD_DTYPE_BF16;
+    return D == 64    ? launch_rows(p, seqs, D, b ? append_kernel<VD_DTYPE_BF16, 64> : append_kernel<VD_DTYPE_F32, 64>, stream)
+           : D == 128 ? launch_rows(p, seqs, D, b ? append_kernel<VD_DTYPE_BF16, 128> : append_kernel<VD_DTYPE_F32, 128>, stream)
+                      : launch_rows(p, seqs, D, b ? append_kernel<VD_DTYPE_BF16, 256> : append_kernel<VD_DTYPE_F32, 256>, stream);
+}
+hipError_t launch_mx_read(const MxRowsParams &p, int seqs, int dtype, int D, hipStream_t stream) {
+    const bool b = dtype == VD_DTYPE_BF16;
+    return D == 64    ? launch_rows(p, seqs, D, b ? read_kernel<VD_DTYPE_BF16, 64> : read_kernel<VD_DTYPE_F32, 64>, stream)
+           : D == 128 ? launch_rows(p, seqs, D, b ? read_kernel<VD_DTYPE_BF16, 128> : read_kernel<VD_DTYPE_F32, 128>, stream)
+                      : launch_rows(p, seqs, D, b ? read_kernel<VD_DTYPE_BF16, 256> : read_kernel<VD_DTYPE_F32, 256>, stream);
+}
+hipError_t launch_mx_attention(const MxAttnParams &p, int seqs, int dtype, int D, hipStream_t stream) {
+    if (dtype == VD_DTYPE_BF16)
+        return D == 64    ? launch_attn<VD_DTYPE_BF16, 64>(p, seqs, stream)
+               : D == 128 ? launch_attn<VD_DTYPE_BF16, 128>(p, seqs, stream)
+                          : launch_attn<VD_DTYPE_BF16, 256>(p, seqs, stream);
+    return D == 64    ? launch_attn<VD_DTYPE_F32, 64>(p, seqs, stream)
+           : D == 128 ? launch_attn<VD_DTYPE_F32, 128>(p, seqs, stream)
+                      : launch_attn<VD_DTYPE_F32, 256>(p, seqs, stream);
+}
+hipError_t launch_mx_evict(const MxEvictParams &p, int seqs, int D, size_t lds, hipStream_t stream) {
+    return D == 64 ? launch_evict<64>(p, seqs, lds, stream)
+           : D == 128 ? launch_evict<128>(p, seqs, lds, stream) : launch_evict<256>(p, seqs, lds, stream);
+}
+
+}  // namespace vd

@@ -8,6 +8,9 @@ optional running-sum state and a ``pos`` payload (the original token index of
 every cached row).  Appending copies the rows into the tail slots: one kernel
 of the HIP library for rows of the cache's type on its GPU, torch's copies for
 any others.  The pass itself runs in the HIP library.
+
+``Mx4EvictingCache`` is the same over a cache held in 4 bits, which also
+attends to it: every step of it runs in the HIP library.
 """
 from typing import Optional, Sequence
 
@@ -67,4 +70,43 @@ class EvictingCache:
                          running_sum=self.running_sum, pos=self.pos, scores_out=scores_out,
                          keep_out=keep_out, num_q_heads=self.num_q_heads, stream=stream,
                          scratch=True)
+        self.n = [min(n, N) for n, N in zip(self.n, self.budget)]
+
+
+class Mx4EvictingCache:
+    """Block prompt processing and decode over a cache held in 4 bits: append,
+    attend (the newest tokens' queries), evict.  ``cache`` is a ``vd.Mx4Cache``."""
+
+    def __init__(self, num_seqs: int, num_layers: int, num_kv_heads: int, head_dim: int,
+                 capacity: int, budget: Sequence[int], device="cuda", variant: str = "l2",
+                 track_pos: bool = True):
+        self.cache = vd.Mx4Cache.zeros(num_seqs, num_layers, num_kv_heads, capacity, head_dim, device)
+        self.units = num_seqs * num_layers * num_kv_heads
+        self.n = [0] * num_seqs          # cached tokens per sequence (host)
+        self.seen = [0] * num_seqs       # tokens appended so far per sequence
+        self.budget = [int(b) for b in budget]
+        self.variant = variant
+        self.pos = (torch.full((self.units, capacity), -1, dtype=torch.int32, device=device)
+                    if track_pos else None)
+        self.capacity = capacity
+
+    def append(self, k_rows: torch.Tensor, v_rows: torch.Tensor, rows: Optional[Sequence[int]] = None):
+        """Appends [seqs, layers, kv_heads, t, head_dim] rows: the first rows[s]
+        of each sequence s (t each where None)."""
+        t = k_rows.shape[3]
+        rows = [t] * len(self.n) if rows is None else [int(r) for r in rows]
+        vd.vd_append_mx4(self.cache, self.n, k_rows, v_rows, rows, self.pos, self.seen)
+        self.n = [n + r for n, r in zip(self.n, rows)]
+        self.seen = [n + r for n, r in zip(self.seen, rows)]
+
+    def attend(self, q: torch.Tensor, rows: Optional[Sequence[int]] = None, scale: Optional[float] = None,
+               out: Optional[torch.Tensor] = None):
+        """Attention of the newest rows[s] tokens of each sequence, q [seqs,
+        layers, q_heads, t, head_dim], over what it caches, themselves included."""
+        return vd.vd_attention_mx4(self.cache, q, self.n, rows, scale, out)
+
+    def evict(self, scores_out=None, keep_out=None, stream=None):
+        """One eviction pass over every unit; afterwards n = min(n, N)."""
+        vd.vd_evict_step_mx4(self.cache, self.n, self.budget, self.variant, pos=self.pos,
+                             scores_out=scores_out, keep_out=keep_out, stream=stream)
         self.n = [min(n, N) for n, N in zip(self.n, self.budget)]

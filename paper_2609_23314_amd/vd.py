@@ -11,8 +11,10 @@ kv_head, head_dim]`` cache is ``x.permute(0, 2, 1, 3).unsqueeze(1)``).
 Per-unit arrays are ``[seq, layer, kv_head, ...]`` contiguous, i.e. unit
 ``u = (s * layers + l) * kv_heads + h``.
 """
+import contextlib
 import ctypes
 import os
+from typing import NamedTuple
 
 import torch
 from torch.autograd import forward_ad
@@ -30,7 +32,9 @@ EXPORTS = ("vd_score", "vd_select_topn", "vd_compact", "vd_evict_step",
            "vd_evict_step_workspace_size", "vd_evict_step_split",
            "vd_evict_step_split_size", "vd_status_string", "vd_stream_read",
            "vd_append", "vd_geometry", "vd_decode_attention_evict", "vd_decode_attention_workspace_size",
-           "vd_decode_attention_evict_noalloc", "vd_decode_attention_noalloc_max_bytes")
+           "vd_decode_attention_evict_noalloc", "vd_decode_attention_noalloc_max_bytes",
+           "vd_append_mx4", "vd_read_mx4", "vd_attention_mx4", "vd_attention_mx4_workspace_size",
+           "vd_evict_step_mx4", "vd_qk_norm_rope")
 
 
 class VdError(RuntimeError):
@@ -49,6 +53,28 @@ class VdCacheDesc(ctypes.Structure):
         ("stride_seq", ctypes.c_int64), ("stride_layer", ctypes.c_int64),
         ("stride_head", ctypes.c_int64), ("stride_slot", ctypes.c_int64),
     ]
+
+
+class VdMx4Cache(ctypes.Structure):
+    _fields_ = [(x, ctypes.c_void_p) for x in ("k", "v", "k_scale", "v_scale")] + [
+        (x, ctypes.c_int32) for x in ("num_seqs", "num_layers", "num_kv_heads", "num_q_heads", "head_dim", "capacity")] + [
+        (x, ctypes.c_int64) for x in ("stride_seq", "stride_layer", "stride_head", "stride_slot",
+                                      "scale_seq", "scale_layer", "scale_head", "scale_slot")]
+
+
+_Strides4 = ctypes.c_int64 * 4
+
+
+class VdRopeSide(ctypes.Structure):
+    _fields_ = [("x", ctypes.c_void_p), ("out", ctypes.c_void_p), ("weight", ctypes.c_void_p),
+                ("strides", _Strides4), ("out_strides", _Strides4),
+                ("heads", ctypes.c_int32), ("out_dtype", ctypes.c_int32)]
+
+
+class VdRopeArgs(ctypes.Structure):
+    _fields_ = [("q", VdRopeSide), ("k", VdRopeSide), ("pos", ctypes.c_void_p), ("inv_freq", ctypes.c_void_p)] + [
+        (x, ctypes.c_int32) for x in ("dtype", "weight_dtype", "num_seqs", "num_layers", "rows", "head_dim", "rotary",
+                                      "interleaved")] + [("eps", ctypes.c_float)]
 
 
 _lib = None
@@ -92,6 +118,16 @@ def load():
     lib.vd_decode_attention_noalloc_max_bytes.argtypes = []
     lib.vd_decode_attention_noalloc_max_bytes.restype = ctypes.c_size_t
     lib.vd_decode_attention_workspace_size.restype = ctypes.c_size_t
+    M = ctypes.POINTER(VdMx4Cache)
+    lib.vd_append_mx4.argtypes = [M, P, P, I32, I32, P, P, P, P, P, P, P]
+    lib.vd_read_mx4.argtypes = [M, P, P, I32, I32, P, P, P, P, P]
+    lib.vd_attention_mx4.argtypes = [M, I32, P, P, I32, P, ctypes.c_float, P, P, P, P, SZ, P]
+    lib.vd_attention_mx4_workspace_size.argtypes = [M, I32, I32, I32]
+    lib.vd_attention_mx4_workspace_size.restype = SZ
+    lib.vd_evict_step_mx4.argtypes = [M, P, P, I32, P, P, P, P]
+    lib.vd_qk_norm_rope.argtypes = [ctypes.POINTER(VdRopeArgs), P]
+    for f in ("vd_append_mx4", "vd_read_mx4", "vd_attention_mx4", "vd_evict_step_mx4", "vd_qk_norm_rope"):
+        getattr(lib, f).restype = ctypes.c_int
     _lib = lib
     return lib
 
@@ -434,6 +470,256 @@ def vd_decode_attention_evict_noalloc(k, v, q, n_valid, budget, running_sum, out
 
 def vd_decode_attention_noalloc_max_bytes():
     return int(load().vd_decode_attention_noalloc_max_bytes())
+
+
+# ------------------------------------------------- a cache in 4 bits, and its rows
+
+class Mx4Cache(NamedTuple):
+    """A KV cache in 4 bits (see "A KV cache held in 4 bits" in vd.h): uint8
+    codes [seq, layer, kv_head, slot, head_dim / 2] and scales [seq, layer,
+    kv_head, slot, head_dim / 32], views of any strides whose last one is 1; k and
+    v alike, k_scale and v_scale alike."""
+    k: torch.Tensor
+    v: torch.Tensor
+    k_scale: torch.Tensor
+    v_scale: torch.Tensor
+
+    @classmethod
+    def zeros(cls, num_seqs, num_layers, num_kv_heads, capacity, head_dim, device="cuda"):
+        shape = (num_seqs, num_layers, num_kv_heads, capacity)
+        return cls(*(torch.zeros((*shape, head_dim // n), dtype=torch.uint8, device=device) for n in (2, 2, 32, 32)))
+
+    def seq(self, s):
+        """The cache of sequence ``s`` alone (a view)."""
+        if not 0 <= s < self.k.shape[0]:
+            raise IndexError(f"no sequence {s}")
+        return Mx4Cache(*(x[s:s + 1] for x in self))
+
+
+def mx4_desc(cache, num_q_heads=None) -> VdMx4Cache:
+    """Descriptor of an ``Mx4Cache``."""
+    k, v, ks, vs = cache
+    shape, sshape, strides, sstrides, dev = k.shape, ks.shape, k.stride(), ks.stride(), k.device
+    if len(shape) != 5 or v.shape != shape or len(sshape) != 5 or vs.shape != sshape:
+        raise ValueError("codes and scales must be 5-D [seq, layer, kv_head, slot, bytes] views, k and v alike")
+    if sshape[:4] != shape[:4] or sshape[4] * 16 != shape[4]:
+        raise ValueError("a row of head_dim channels has head_dim / 2 bytes of codes and head_dim / 32 of scales")
+    if v.stride() != strides or vs.stride() != sstrides or strides[4] != 1 or (sstrides[4] != 1 and sshape[4] > 1):
+        raise ValueError("k and v must have the same strides, and the last one must be 1")
+    for t in cache:
+        if t.dtype != torch.uint8 or t.device != dev or not t.is_cuda:
+            raise ValueError("codes and scales must be uint8 tensors on one GPU")
+    S, L, H, C, B = shape
+    return VdMx4Cache(k.data_ptr(), v.data_ptr(), ks.data_ptr(), vs.data_ptr(), S, L, H,
+                      H if num_q_heads is None else int(num_q_heads), 2 * B, C, *strides[:4], *sstrides[:4])
+
+
+def _no_grad(name, *tensors):
+    """These calls have no backward: an input that asks for one is refused."""
+    if torch.is_grad_enabled():
+        for t in tensors:
+            if t is not None and t.requires_grad:
+                raise ValueError(f"{name} has no gradient: detach its inputs or call it under torch.no_grad()")
+
+
+def _rows_view(x, name, shape, dtype, dev):
+    """A 5-D [seq, layer, head, row, head_dim] view as pointer and strides."""
+    if x.dim() != 5 or x.shape != shape or x.device != dev or x.dtype != dtype or x.is_neg():
+        raise ValueError(f"{name} must be a {dtype} tensor {list(shape)} on {dev}")
+    strides = x.stride()
+    if strides[4] != 1:
+        raise ValueError(f"{name}: the head_dim stride must be 1")
+    # (an axis of one element is never stepped along, whatever its stride says)
+    return x.data_ptr(), _Strides4(*(st if n > 1 else 0 for st, n in zip(strides[:4], shape)))
+
+
+_same_device = contextlib.nullcontext()
+
+
+def _on(dev):
+    """The device of the call's tensors made the current one, where it is not."""
+    return _same_device if torch._C._cuda_getDevice() == dev.index else torch.cuda.device(dev)
+
+
+def _stream_context(dev, stream):
+    """The caller's stream made torch's current one, so that what a call allocates
+    belongs to it."""
+    if stream is None:
+        return _same_device
+    if isinstance(stream, torch.cuda.Stream):
+        return torch.cuda.stream(stream)
+    handle = stream.cuda_stream
+    return torch.cuda.stream(torch.cuda.ExternalStream(handle, dev) if handle else torch.cuda.default_stream(dev))
+
+
+def _moved(*tensors):
+    """torch's backward refuses tensors whose version moved since it saved them."""
+    torch._C._increment_version(tuple(t for t in tensors if t is not None and not t.is_inference()))
+
+
+def vd_append_mx4(cache, n_old, k_rows, v_rows, rows=None, pos=None, pos0=None, *, stream=None):
+    """Rows [S, L, H, t, D] (bfloat16 or float32) into slots [n_old[s], n_old[s] +
+    rows[s]) of every unit, in 4 bits (see ``vd_append_mx4`` in vd.h); rows: t
+    each where None.  pos: int32 [U, capacity], given pos0[s] + r (pos0: n_old)."""
+    _no_grad("vd_append_mx4", k_rows, v_rows)
+    desc = mx4_desc(cache)
+    S, L, H, C, _ = cache.k.shape
+    dev, t = cache.k.device, k_rows.shape[3] if k_rows.dim() == 5 else 0
+    shape = (S, L, H, t, desc.head_dim)
+    kp, ks = _rows_view(k_rows, "k_rows", shape, k_rows.dtype, dev)
+    vp, vs = _rows_view(v_rows, "v_rows", shape, k_rows.dtype, dev)
+    if pos is not None:
+        _need(pos, "pos", torch.int32, S * L * H * C, dev)
+    n_h = _host_i32(n_old, S, "n_old")
+    r_h = None if rows is None else _host_i32(rows, S, "rows")
+    p_h = None if pos0 is None else _host_i32(pos0, S, "pos0")
+    with _on(dev):
+        _check("vd_append_mx4", load().vd_append_mx4(
+            ctypes.byref(desc), _ptr(n_h), _ptr(r_h), t, _dtype_code(k_rows), kp, ks, vp, vs, _ptr(pos), _ptr(p_h),
+            _stream(dev, stream)))
+    _moved(*cache, pos)
+
+
+def vd_read_mx4(cache, first, t, rows=None, k_out=None, v_out=None, *, dtype=torch.bfloat16, stream=None):
+    """The values of slots [first[s], first[s] + rows[s]) of every unit (see
+    ``vd_read_mx4`` in vd.h); returns (k, v), [S, L, H, t, D] of ``dtype`` or the
+    given outputs.  rows: t each where None; others are left as they were."""
+    desc = mx4_desc(cache)
+    S, L, H = cache.k.shape[:3]
+    dev, shape = cache.k.device, (S, L, H, int(t), desc.head_dim)
+    n_h = _host_i32(first, S, "first")
+    r_h = None if rows is None else _host_i32(rows, S, "rows")
+    with _on(dev):
+        if k_out is None or v_out is None:
+            with _stream_context(dev, stream):
+                k_out = torch.empty(shape, dtype=dtype, device=dev) if k_out is None else k_out
+                v_out = torch.empty(shape, dtype=dtype, device=dev) if v_out is None else v_out
+        _no_grad("vd_read_mx4", k_out, v_out)
+        kp, ks = _rows_view(k_out, "k_out", shape, k_out.dtype, dev)
+        vp, vs = _rows_view(v_out, "v_out", shape, k_out.dtype, dev)
+        _check("vd_read_mx4", load().vd_read_mx4(ctypes.byref(desc), _ptr(n_h), _ptr(r_h), shape[3], _dtype_code(k_out),
+                                                 kp, ks, vp, vs, _stream(dev, stream)))
+    _moved(k_out, v_out)
+    return k_out, v_out
+
+
+def vd_attention_mx4_workspace_size(cache, num_q_heads, t, n=None, dtype=torch.bfloat16):
+    """Bytes of workspace for ``t`` query rows a sequence over at most n cached
+    tokens (None: the cache's capacity)."""
+    desc = mx4_desc(cache, num_q_heads)
+    code = VD_DTYPE_BF16 if dtype == torch.bfloat16 else VD_DTYPE_F32
+    return int(load().vd_attention_mx4_workspace_size(ctypes.byref(desc), code, int(t), desc.capacity if n is None else int(n)))
+
+
+def vd_attention_mx4(cache, q, n_valid, rows=None, scale=None, out=None, workspace=None, *, stream=None):
+    """Attention of the newest tokens over a 4-bit cache (see ``vd_attention_mx4``
+    in vd.h): q is [S, L, Hq, t, D], bfloat16 or float32, any strides whose last
+    one is 1; returns the output, q's shape and type.  Query row i of rows[s] (t
+    where None) sees the slots j < n_valid[s] - rows[s] + 1 + i.  Without a
+    workspace the call takes its own from torch."""
+    _no_grad("vd_attention_mx4", q, out)
+    if q.dim() != 5:
+        raise ValueError("q must be [S, L, Hq, t, D] matching the cache")
+    S, L, H = cache.k.shape[:3]
+    Hq, t = q.shape[2], q.shape[3]
+    desc = mx4_desc(cache, Hq)
+    dev, shape = cache.k.device, (S, L, Hq, t, desc.head_dim)
+    qp, qs = _rows_view(q, "q", shape, q.dtype, dev)
+    code = _dtype_code(q)
+    n_h = _host_i32(n_valid, S, "n_valid")
+    r_h = None if rows is None else _host_i32(rows, S, "rows")
+    sc = float(desc.head_dim) ** -0.5 if scale is None else float(scale)
+    with _on(dev):
+        size = 0
+        if workspace is None:
+            longest = max(n_h) if isinstance(n_h, ctypes.Array) else int(n_h.max())
+            size = load().vd_attention_mx4_workspace_size(ctypes.byref(desc), code, t, min(max(longest, 0), desc.capacity))
+        if out is None or size:
+            with _stream_context(dev, stream):
+                out = torch.empty(shape, dtype=q.dtype, device=dev) if out is None else out
+                workspace = torch.empty(size, dtype=torch.uint8, device=dev) if size else workspace
+        if workspace is not None:
+            _need(workspace, "workspace", torch.uint8, 0, dev)
+        op, os_ = _rows_view(out, "out", shape, q.dtype, dev)
+        _check("vd_attention_mx4", load().vd_attention_mx4(
+            ctypes.byref(desc), code, qp, qs, t, _ptr(r_h), sc, _ptr(n_h), op, os_, _ptr(workspace),
+            0 if workspace is None else workspace.numel(), _stream(dev, stream)))
+    _moved(out)
+    return out
+
+
+def vd_evict_step_mx4(cache, n_valid, budget, variant="l2", pos=None, scores_out=None, keep_out=None, *, stream=None):
+    """One eviction pass over every unit of a 4-bit cache, in place (see
+    ``vd_evict_step_mx4`` in vd.h)."""
+    desc = mx4_desc(cache)
+    S, L, H, C, _ = cache.k.shape
+    dev, U = cache.k.device, S * L * H
+    n_h = _host_i32(n_valid, S, "n_valid")
+    b_h = _host_i32(budget, S, "budget")
+    if pos is not None:
+        _need(pos, "pos", torch.int32, U * C, dev)
+    if scores_out is not None:
+        _need(scores_out, "scores_out", torch.float32, U * C, dev)
+    if keep_out is not None:
+        _need(keep_out, "keep_out", torch.uint8, U * C, dev)
+    with _on(dev):
+        _check("vd_evict_step_mx4", load().vd_evict_step_mx4(
+            ctypes.byref(desc), _ptr(n_h), _ptr(b_h), VARIANTS[variant], _ptr(pos), _ptr(scores_out), _ptr(keep_out),
+            _stream(dev, stream)))
+    _moved(*cache, pos, scores_out, keep_out)
+
+
+def _rope_side(x, out, weight, name, S, L, t, D, w_dtype):
+    if x is None:
+        return VdRopeSide()
+    dev, shape = x.device, (S, L, x.shape[2], t, D)
+    xp, xs = _rows_view(x, name, shape, x.dtype, dev)
+    op, os_ = _rows_view(out, name + "_out", shape, out.dtype, dev)
+    if weight is not None:
+        _need(weight, name + "_weight", w_dtype, L * D, dev)
+        if weight.numel() != L * D:
+            raise ValueError(f"{name}_weight must be [layers, head_dim]")
+    return VdRopeSide(xp, op, _ptr(weight), xs, os_, shape[2], _dtype_code(out))
+
+
+def vd_qk_norm_rope(q, k, pos, inv_freq, q_weight=None, k_weight=None, q_out=None, k_out=None, *, eps=1e-6,
+                    interleaved=False, stream=None):
+    """Norm of each head's query and key rows and their rotation (see
+    ``vd_qk_norm_rope`` in vd.h): q [S, L, Hq, t, D] and k [S, L, H, t, D],
+    bfloat16 or float32, any strides whose last one is 1, either of them None; pos
+    int32 [S, t]; inv_freq float32 [rotary / 2]; weights [L, D], None for no norm.
+    Returns (q_out, k_out): new tensors of the inputs' type, or the given ones
+    (either type; the input itself for a call in place, or the cache's own slots)."""
+    some = q if q is not None else k
+    if some is None or some.dim() != 5:
+        raise ValueError("q or k must be given, [S, L, heads, t, D]")
+    _no_grad("vd_qk_norm_rope", q, k, q_weight, k_weight, q_out, k_out)
+    S, L, _, t, D = some.shape
+    dev = some.device
+    if not some.is_cuda:
+        raise ValueError("q and k must be on a GPU")
+    if q is not None and k is not None and (k.dim() != 5 or k.dtype != q.dtype or k.device != dev):
+        raise ValueError("k must match q in type and device")
+    if (q is None and q_out is not None) or (k is None and k_out is not None):
+        raise ValueError("an output without its input")
+    _need(pos, "pos", torch.int32, S * t, dev)
+    if pos.numel() != S * t:
+        raise ValueError("pos must be [seqs, rows]")
+    _need(inv_freq, "inv_freq", torch.float32, 0, dev)
+    w = q_weight if q_weight is not None else k_weight
+    with _on(dev):
+        if (q is not None and q_out is None) or (k is not None and k_out is None):
+            with _stream_context(dev, stream):
+                q_out = torch.empty(q.shape, dtype=q.dtype, device=dev) if q is not None and q_out is None else q_out
+                k_out = torch.empty(k.shape, dtype=k.dtype, device=dev) if k is not None and k_out is None else k_out
+        w_dtype = some.dtype if w is None else w.dtype
+        args = VdRopeArgs(_rope_side(q, q_out, q_weight, "q", S, L, t, D, w_dtype),
+                          _rope_side(k, k_out, k_weight, "k", S, L, t, D, w_dtype), pos.data_ptr(), inv_freq.data_ptr(),
+                          _dtype_code(some), VD_DTYPE_F32 if w is None else _dtype_code(w), S, L, t, D,
+                          2 * inv_freq.numel(), bool(interleaved), float(eps))
+        _check("vd_qk_norm_rope", load().vd_qk_norm_rope(ctypes.byref(args), _stream(dev, stream)))
+    _moved(q_out, k_out)
+    return q_out, k_out
 
 
 def vd_stream_read(buf, sink, *, stream=None):

@@ -1,0 +1,512 @@
+"""The 4-bit cache on the GPU against its definitions in 64 bits (mx4_ref.py):
+append and read, attention, the eviction pass, and a run of them together."""
+import math
+
+import pytest
+import torch
+
+import mx4_ref as ref
+from paper_2609_23314_amd import vd
+from paper_2609_23314_amd.driver import Mx4EvictingCache
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+
+
+def _rows(shape, dtype, seed, spread=1.0):
+    """Rows whose channels and tokens differ in size."""
+    g = torch.Generator().manual_seed(seed)
+    x = torch.randn(shape, generator=g) * torch.exp(spread * torch.randn((*shape[:-2], 1, shape[-1]), generator=g))
+    return (x * torch.where(torch.rand((*shape[:-1], 1), generator=g) < 0.05, 8.0, 1.0)).to(dtype)
+
+
+def _cache(S, L, H, C, D, seed, nhd=False):
+    """A cache of quantised rows; nhd: an engine's [seq, slot, head, bytes] layout, padded."""
+    made = []
+    for i in (0, 1):
+        made.append(ref.encode(_rows((S, L, H, C, D), torch.float32, seed + i)))
+    def place(x):
+        if not nhd:
+            return x.to(DEV)
+        B = x.shape[-1]
+        y = torch.full((S, L, C, H, 2 * B), 0xEE, dtype=torch.uint8, device=DEV)[..., :B].permute(0, 1, 3, 2, 4)
+        y.copy_(x)
+        return y
+    return vd.Mx4Cache(place(made[0][0]), place(made[1][0]), place(made[0][1]), place(made[1][1]))
+
+
+# ------------------------------------------------------------------ append and read
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("D", [64, 128, 256])
+@pytest.mark.parametrize("S,L,H,t", [(1, 1, 1, 1), (3, 2, 3, 5), (2, 1, 2, 133)])
+def test_append_and_read(dtype, D, S, L, H, t):
+    C = t + 9
+    cache = Mx4EvictingCache(S, L, H, D, C, [C] * S, device=DEV)
+    for x in cache.cache:
+        x.fill_(0xA5)
+    k, v = _rows((S, L, H, t, D), dtype, 1), _rows((S, H, L, t, D), dtype, 2).transpose(1, 2)
+    n_old = [(3 * s) % 9 for s in range(S)]
+    rows = [t if s != 1 else t // 2 for s in range(S)]
+    cache.n, cache.seen = list(n_old), [100 + s for s in range(S)]
+    cache.append(k.to(DEV), v.to(DEV).transpose(1, 2).contiguous().transpose(1, 2), rows)
+    torch.cuda.synchronize()
+    got = [x.cpu() for x in cache.cache]
+    want = [ref.encode(x) for x in (k, v)]
+    for s in range(S):
+        a, b = n_old[s], n_old[s] + rows[s]
+        for i in (0, 1):
+            assert torch.equal(got[i][s, :, :, a:b], want[i][0][s, :, :, :rows[s]])
+            assert torch.equal(got[2 + i][s, :, :, a:b], want[i][1][s, :, :, :rows[s]])
+            for x in (got[i], got[2 + i]):   # the slots around them are as they were
+                assert x[s, :, :, :a].eq(0xA5).all() and x[s, :, :, b:].eq(0xA5).all()
+        pos = cache.pos.cpu().view(S, L, H, C)[s]
+        assert torch.equal(pos[:, :, a:b], torch.arange(100 + s, 100 + s + rows[s]).expand(L, H, -1).int())
+        assert pos[:, :, :a].eq(-1).all() and pos[:, :, b:].eq(-1).all()
+    assert cache.n == [n + r for n, r in zip(n_old, rows)]
+    for out_dtype in (torch.bfloat16, torch.float32):
+        outs = [torch.full((S, L, H, t, D), 77.0, dtype=out_dtype, device=DEV) for _ in range(2)]
+        vd.vd_read_mx4(cache.cache, n_old, t, rows, *outs)
+        for i in (0, 1):
+            for s in range(S):
+                assert torch.equal(outs[i][s, :, :, :rows[s]].cpu().double(), ref.decode(want[i][0], want[i][1])[s, :, :, :rows[s]])
+                assert outs[i][s, :, :, rows[s]:].eq(77).all()
+
+
+def test_append_borders():
+    """Ties, the scale's steps, the largest and smallest values, signed zeros, and groups with NaN or infinities."""
+    rows = []
+    for e in (-149, -130, -128, -127, -126, -20, 0, 1, 100, 125, 127):
+        for top in (3.5, 6.0, 6.9999995, 7.0, 7.5, 1.0):
+            x = torch.linspace(-1.0, 1.0, 32).double() * 6
+            x[:12] = torch.tensor([0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0, -0.25, -0.75, -2.5, -5.0, -0.0]).double()
+            x[12] = top
+            x = (x.clamp(-top, top) * 2.0 ** e)
+            rows.append(x.clamp(-3.4e38, 3.4e38).float())
+    for bad in (math.nan, math.inf, -math.inf):
+        x = torch.ones(32)
+        x[5] = bad
+        rows.append(x)
+    rows.append(torch.zeros(32))
+    rows.append(-torch.zeros(32))
+    x = torch.stack(rows)
+    x = torch.cat([x, x[: (-len(x)) % 4]]).view(1, 1, 1, -1, 128)
+    for dtype in (torch.float32, torch.bfloat16):
+        y = x.to(dtype)
+        t = y.shape[3]
+        cache = vd.Mx4Cache.zeros(1, 1, 1, t, 128, DEV)
+        vd.vd_append_mx4(cache, [0], y.to(DEV), y.to(DEV))
+        codes, scales = ref.encode(y)
+        assert torch.equal(cache.k_scale.cpu(), scales) and torch.equal(cache.v_scale.cpu(), scales)
+        assert torch.equal(cache.k.cpu(), codes) and torch.equal(cache.v.cpu(), codes)
+        back = vd.vd_read_mx4(cache, [0], t, dtype=torch.float32)[0].cpu().double()
+        want = ref.decode(codes, scales)
+        assert torch.equal(back.isnan(), want.isnan()) and torch.equal(back.nan_to_num(), want.nan_to_num())
+        bad = (~torch.isfinite(y)).unflatten(-1, (-1, 32)).any(-1).repeat_interleave(32, -1)   # (bf16 rounds the largest to infinity)
+        assert torch.isfinite(want[~bad]).all() and torch.equal(want.isnan(), bad) and bad.sum() >= 3 * 32
+
+
+def test_append_many_sequences():
+    """More sequences than one launch takes."""
+    S, D = 259, 64
+    k = _rows((S, 1, 2, 3, D), torch.bfloat16, 5)
+    cache = vd.Mx4Cache.zeros(S, 1, 2, 8, D, DEV)
+    n_old, rows = [s % 5 for s in range(S)], [s % 4 for s in range(S)]
+    pos = torch.full((S * 2, 8), -1, dtype=torch.int32, device=DEV)
+    vd.vd_append_mx4(cache, n_old, k.to(DEV), k.to(DEV), rows, pos)
+    codes, scales = ref.encode(k)
+    want = torch.zeros((S, 1, 2, 8, D // 2), dtype=torch.uint8)
+    wpos = torch.full((S, 2, 8), -1, dtype=torch.int32)
+    for s in range(S):
+        want[s, :, :, n_old[s]:n_old[s] + rows[s]] = codes[s, :, :, :rows[s]]
+        wpos[s, :, n_old[s]:n_old[s] + rows[s]] = torch.arange(n_old[s], n_old[s] + rows[s])
+    assert torch.equal(cache.v.cpu(), want) and torch.equal(pos.cpu().view(S, 2, 8), wpos)
+
+
+# ------------------------------------------------------------------ attention
+
+def _check_attention(cache, q, n, rows, out, scale):
+    """Each output within what its roundings allow.  With u the rounding of a
+    weight (bf16 2^-8, two parts 2^-16): products are exact, a logit is a sum of D
+    fp32 terms, taken for D * 2^-23 of the sum of their sizes (the matrix cores may
+    cut rather than round); an exponential is off by a few fp32 steps, a sum of n
+    weighted values by n * 2^-24 at most; numerator and denominator alike.  Weights
+    are relative to a logit at most 8 (log2 units) below the row's largest, and so
+    is what one wave's sums are multiplied by: where either is below 2^-126 (fp32
+    and bf16 have no smaller normal number) it counts as 0, which loses at most n *
+    2^8 * 2^-126 of the largest |v|, against a denominator of at least 1."""
+    S, L, H, C, D = cache.k.shape
+    D *= 2
+    G = q.shape[2] // H
+    u = 2.0 ** -8 if q.dtype == torch.bfloat16 else 2.0 ** -16
+    eps = torch.finfo(q.dtype).eps / 2
+    kd, vdec = ref.decode(cache.k, cache.k_scale), ref.decode(cache.v, cache.v_scale)
+    got, qd = out.cpu().double(), q.cpu().double()
+    worst = 0.0
+    for s in range(S):
+        for l in range(L):
+            for h in range(H):
+                hs = slice(h * G, (h + 1) * G)
+                want, size, prod = ref.attention(kd[s, l, h], vdec[s, l, h], qd[s, l, hs], n[s], rows[s], scale)
+                dz = (D * 2.0 ** -23 + 2.0 ** -22) * abs(scale) * prod
+                tol = 2 * (u + 2 * dz + (max(n[s], 1) + 16) * 2.0 ** -24) * size
+                tol = tol + 2 * n[s] * 2.0 ** -118 * vdec[s, l, h, :n[s]].abs().max() if n[s] else tol
+                tol = tol + eps * (want.abs() + tol)
+                err = (got[s, l, hs] - want).abs()[:, :rows[s]]
+                assert (err <= tol[:, :rows[s]]).all(), (s, l, h, float(err.max()))
+                worst = max(worst, float((err / tol[:, :rows[s]]).max()) if err.numel() else 0.0)
+    return worst
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("D", [64, 128, 256])
+@pytest.mark.parametrize("G,n", [(1, [1, 0]), (4, [31, 33]), (3, [129, 128]), (8, [1000, 257]), (16, [5, 600]), (40, [70, 300])])
+def test_attention_single_tokens(dtype, D, G, n):
+    S, L, H, C = 2, 1, 2, max(n) + 3
+    cache = _cache(S, L, H, C, D, 11)
+    q = _rows((S, L, H * G, 1, D), dtype, 13, 0.3).to(DEV)
+    out = vd.vd_attention_mx4(cache, q, n)
+    assert out.dtype == dtype and out.shape == q.shape
+    _check_attention(cache, q, n, [1] * S, out, D ** -0.5)
+    for s in range(S):
+        if n[s] == 0:
+            assert not out[s].any()
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("D,G,t,n", [(64, 1, 2, 2), (64, 4, 33, 40), (64, 5, 100, 731), (128, 1, 65, 65), (128, 4, 16, 300),
+                                     (128, 3, 77, 1030), (128, 8, 40, 513), (256, 2, 31, 100), (256, 1, 130, 450), (256, 7, 19, 259)])
+def test_attention_blocks(dtype, D, G, t, n):
+    """Blocks of query rows: causal within the block, ragged ones, and one longer
+    than what is cached, whose first rows see nothing."""
+    S, L, H = 3, 2, 1
+    cache = _cache(S, L, H, n, D, 21)
+    q = _rows((S, L, H * G, t, D), dtype, 23, 0.3).to(DEV)
+    ns, rows = [n, max(1, n // 2), max(0, t // 2)], [t, max(1, t - 1), t]
+    rows[1] = min(rows[1], ns[1])
+    out = torch.full((S, L, H * G, t, D), 55.0, dtype=dtype, device=DEV)
+    assert vd.vd_attention_mx4(cache, q, ns, rows, scale=0.11, out=out) is out
+    _check_attention(cache, q, ns, rows, out, 0.11)
+    assert out[1, :, :, rows[1]:].eq(55).all()
+    empty = rows[2] - ns[2]          # rows that see nothing
+    assert empty > 0 and not out[2, :, :, :empty].any() and out[2, :, :, empty:].any()
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("t", [1, 50])
+def test_attention_layouts(dtype, t):
+    """An engine's layouts: padded [seq, slot, head] caches, [token, head * D] queries and outputs, layers shared."""
+    S, L, H, G, C, D = 2, 2, 3, 2, 300, 128
+    cache = _cache(S, L, H, C, D, 31, nhd=True)
+    base = _rows((S, t, L, 3 * H * G, D), dtype, 33, 0.3).to(DEV)
+    q = base[:, :, :, H * G:2 * H * G].permute(0, 2, 3, 1, 4)
+    out = torch.zeros((S, t, L, H * G, D), dtype=dtype, device=DEV).permute(0, 2, 3, 1, 4)
+    n = [300, 211]
+    vd.vd_attention_mx4(cache, q, n, out=out)
+    _check_attention(cache, q, n, [t] * S, out, D ** -0.5)
+    shared = vd.Mx4Cache(*(x[:1].expand(S, -1, -1, -1, -1) for x in cache))   # a prompt that two sequences share
+    out2 = vd.vd_attention_mx4(shared, q, n)
+    _check_attention(vd.Mx4Cache(*(x.contiguous() for x in shared)), q, n, [t] * S, out2, D ** -0.5)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_attention_long_split(dtype):
+    """A long sequence, split over workgroups, in a workspace of the call's own and in a given one of any content."""
+    H, G, n, D = 2, 4, 20011, 128
+    cache = _cache(1, 1, H, n, D, 41)
+    q = _rows((1, 1, H * G, 1, D), dtype, 43, 0.3).to(DEV)
+    size = vd.vd_attention_mx4_workspace_size(cache, H * G, 1, dtype=dtype)
+    assert size > 0
+    out = vd.vd_attention_mx4(cache, q, [n])
+    _check_attention(cache, q, [n], [1], out, D ** -0.5)
+    given = torch.full((size,), 0xFF, dtype=torch.uint8, device=DEV)
+    assert torch.equal(vd.vd_attention_mx4(cache, q, [n], workspace=given), out)
+    # a short sequence in the same cache, in the same workspace
+    _check_attention(cache, q, [777], [1], vd.vd_attention_mx4(cache, q, [777], workspace=given), D ** -0.5)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("t", [1, 40])
+def test_attention_extreme_logits(dtype, t):
+    """Logits in the hundreds, growing and falling along the rows; a weight of one."""
+    H, G, n, D = 1, 4, 700, 128
+    k = _rows((1, 1, H, n, D), torch.float32, 51) * torch.linspace(0.1, 30, n).view(n, 1)
+    for rows_k in (k, k.flip(3)):
+        cache = vd.Mx4Cache.zeros(1, 1, H, n, D, DEV)
+        vd.vd_append_mx4(cache, [0], rows_k.to(DEV), _rows((1, 1, H, n, D), torch.float32, 52).to(DEV))
+        q = _rows((1, 1, H * G, t, D), dtype, 53).to(DEV)
+        out = vd.vd_attention_mx4(cache, q, [n])
+        assert torch.isfinite(out).all()
+        _check_attention(cache, q, [n], [t], out, D ** -0.5)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("D", [64, 128, 256])
+@pytest.mark.parametrize("side", [0, 1])
+@pytest.mark.parametrize("t,G", [(6, 2), (70, 1)])
+def test_attention_nan_rows_stay_with_their_queries(dtype, D, side, t, G):
+    """A row with a NaN group reaches the queries that see it and no other; rows
+    behind the cached ones, of any bytes, reach none."""
+    n, bad = 100, 97
+    cache = _cache(1, 1, 1, n + 28, D, 61)
+    for x in cache[:2]:
+        x[:, :, :, n:] = 0x77
+    for x in cache[2:]:
+        x[:, :, :, n:] = 255
+    q = _rows((1, 1, G, t, D), dtype, 63, 0.3).to(DEV)
+    clean = vd.vd_attention_mx4(cache, q, [n])
+    assert torch.isfinite(clean).all()
+    _check_attention(vd.Mx4Cache(*(x[:, :, :, :n] for x in cache)), q, [n], [t], clean, D ** -0.5)
+    cache[2 + side][0, 0, 0, bad, D // 32 - 1] = 255
+    out = vd.vd_attention_mx4(cache, q, [n])
+    sees = torch.tensor([bad < n - t + 1 + i for i in range(t)], device=DEV)
+    assert out[:, :, :, sees].isnan().all() and torch.equal(out[:, :, :, ~sees], clean[:, :, :, ~sees])
+
+
+def test_attention_nonfinite_queries():
+    """A query row with NaN or an infinity spoils its own output alone."""
+    cache = _cache(1, 1, 1, 200, 128, 65)
+    for dtype in (torch.bfloat16, torch.float32):
+        for t in (3, 30):
+            q = _rows((1, 1, 2, t, 128), dtype, 66, 0.3).to(DEV)
+            clean = vd.vd_attention_mx4(cache, q, [200])
+            for x in (math.nan, math.inf):
+                p = q.clone()
+                p[0, 0, 1, 2, 7] = x
+                out = vd.vd_attention_mx4(cache, p, [200])
+                assert out[0, 0, 1, 2].isnan().all()
+                out[0, 0, 1, 2] = clean[0, 0, 1, 2]
+                assert torch.equal(out, clean)
+
+
+def test_attention_far_slots():
+    """Byte offsets past 31 bits within a unit and past 32 between units."""
+    C, D, H = 150000, 256, 2
+    strides = (0, 0, C * 16384 + 4096, 16384, 1)
+    sstrides = (0, 0, C * 64 + 8, 64, 1)
+    base = torch.zeros(2 * (C * 16384 + 4096) + 64, dtype=torch.uint8, device=DEV)
+    codes = [base.as_strided((1, 1, H, C, D // 2), strides, off) for off in (0, 128)]
+    sbase = [torch.zeros(2 * (C * 64 + 8), dtype=torch.uint8, device=DEV) for _ in range(2)]
+    cache = vd.Mx4Cache(*codes, *(x.as_strided((1, 1, H, C, D // 32), sstrides) for x in sbase))
+    t = 130
+    k, v = _rows((1, 1, H, t, D), torch.float32, 71), _rows((1, 1, H, t, D), torch.float32, 72)
+    vd.vd_append_mx4(cache, [C - t], k.to(DEV), v.to(DEV))
+    # all other rows are zero: zero keys and zero values
+    back = vd.vd_read_mx4(cache, [C - t], t, dtype=torch.float32)
+    for x, y in zip(back, (k, v)):
+        assert torch.equal(x.cpu().double(), ref.decode(*ref.encode(y)))
+    q = _rows((1, 1, H, 1, D), torch.float32, 73, 0.3).to(DEV)
+    out = vd.vd_attention_mx4(cache, q, [C]).cpu().double()
+    for h in range(H):
+        z = (q[0, 0, h].cpu().double() @ ref.decode(*ref.encode(k))[0, 0, h].T / 16).squeeze(0)
+        w = torch.exp(z - z.max())
+        total = w.sum() + (C - t) * torch.exp(-z.max())
+        want = w @ ref.decode(*ref.encode(v))[0, 0, h] / total
+        assert (out[0, 0, h, 0] - want).abs().max() <= 1e-4 * want.abs().max()
+    del base, sbase, cache
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("t", [1, 33])
+def test_attention_many_sequences(dtype, t):
+    """More sequences than one launch takes, each of its own length."""
+    S, D = 260, 64
+    cache = _cache(S, 1, 1, 40, D, 81)
+    q = _rows((S, 1, 2, t, D), dtype, 83, 0.3).to(DEV)
+    n, rows = [s % 41 for s in range(S)], [(s * 7) % (t + 1) for s in range(S)]
+    out = torch.zeros((S, 1, 2, t, D), dtype=dtype, device=DEV)
+    vd.vd_attention_mx4(cache, q, n, rows, out=out)
+    _check_attention(cache, q, n, rows, out, D ** -0.5)
+
+
+# ------------------------------------------------------------------ eviction
+
+def _check_evict(cache, before, n, N, variant, scores, keep, pos):
+    S, L, H, C, B = before[0].shape
+    after = [x.cpu() for x in cache]
+    scores, keep, pos = scores.cpu().view(S, L, H, C), keep.cpu().view(S, L, H, C), pos.cpu().view(S, L, H, C)
+    values = ref.decode(before[0], before[2]) if variant.startswith("key") else ref.decode(before[1], before[3])
+    for s in range(S):
+        for l in range(L):
+            for h in range(H):
+                m = n[s]
+                want = ref.scores(values[s, l, h, :m], variant) if m else torch.zeros(0).double()
+                got = scores[s, l, h]
+                # one rounding to fp32, of a value that fp64 has to about 1e-15 of its terms
+                assert ((got[:m].double() - want).abs() <= 2.0 ** -24 * want.abs() + 1e-14 * (1 + want.abs())).all()
+                assert got[m:].eq(-9).all() and keep[s, l, h, m:].eq(7).all()
+                stay = ref.kept(got[:m].tolist(), N[s], variant) if m > N[s] else list(range(m))
+                mask = torch.zeros(m, dtype=torch.uint8)
+                mask[stay] = 1
+                assert torch.equal(keep[s, l, h, :m], mask), (s, l, h)
+                slots = torch.arange(C)
+                for a, b in ref.moves(stay, m, N[s]):
+                    slots[b] = a
+                for x, y in zip(after, before):
+                    assert torch.equal(x[s, l, h], y[s, l, h, slots])
+                assert torch.equal(pos[s, l, h], slots.int())
+
+
+@pytest.mark.parametrize("variant", ["l2", "dir", "norm", "key_l2", "key_dir", "key_norm"])
+@pytest.mark.parametrize("D", [64, 128, 256])
+@pytest.mark.parametrize("n,N", [([1, 2, 0], [1, 1, 5]), ([33, 65, 64], [32, 10, 64]), ([300, 257, 90], [200, 256, 1]),
+                                 ([1100, 1025, 2048], [1024, 1000, 40])])
+def test_evict(variant, D, n, N):
+    S, L, H, C = 3, 1, 2, max(n) + 2
+    cache = _cache(S, L, H, C, D, 91)
+    before = [x.cpu().clone() for x in cache]
+    pos = torch.arange(C, dtype=torch.int32, device=DEV).repeat(S * L * H, 1)
+    scores = torch.full((S * L * H, C), -9.0, device=DEV)
+    keep = torch.full((S * L * H, C), 7, dtype=torch.uint8, device=DEV)
+    vd.vd_evict_step_mx4(cache, n, N, variant, pos=pos, scores_out=scores, keep_out=keep)
+    _check_evict(cache, before, n, N, variant, scores, keep, pos)
+
+
+@pytest.mark.parametrize("variant", ["l2", "dir", "norm", "key_norm"])
+@pytest.mark.parametrize("n,N", [(400, 399), (400, 150), (1500, 1100)])
+def test_evict_ties(variant, n, N):
+    """Rows that repeat often, and rows of zeros."""
+    D, H = 64, 3
+    few = _rows((5, D), torch.float32, 95)
+    few[3] = 0
+    pick = torch.randint(0, 5, (1, 1, H, n), generator=torch.Generator().manual_seed(96))
+    pick[0, 0, 2] = 3                                   # a unit of zeros
+    x = few[pick]
+    cache = vd.Mx4Cache.zeros(1, 1, H, n, D, DEV)
+    vd.vd_append_mx4(cache, [0], x.to(DEV), x.to(DEV))
+    before = [y.cpu().clone() for y in cache]
+    pos = torch.arange(n, dtype=torch.int32, device=DEV).repeat(H, 1)
+    scores, keep = torch.full((H, n), -9.0, device=DEV), torch.full((H, n), 7, dtype=torch.uint8, device=DEV)
+    vd.vd_evict_step_mx4(cache, [n], [N], variant, pos=pos, scores_out=scores, keep_out=keep)
+    _check_evict(cache, before, [n], [N], variant, scores, keep, pos)
+
+
+@pytest.mark.parametrize("N", [16383, 8192, 100])
+def test_evict_full_capacity(N):
+    """The most slots, in an engine's layout, with and without the optional outputs."""
+    C, D = vd.MAX_CAPACITY, 64
+    cache = _cache(1, 1, 2, C, D, 97, nhd=True)
+    before = [x.cpu().clone() for x in cache]
+    twin = vd.Mx4Cache(*(x.clone(memory_format=torch.preserve_format) for x in cache))
+    pos = torch.arange(C, dtype=torch.int32, device=DEV).repeat(2, 1)
+    scores, keep = torch.full((2, C), -9.0, device=DEV), torch.full((2, C), 7, dtype=torch.uint8, device=DEV)
+    vd.vd_evict_step_mx4(cache, [C], [N], pos=pos, scores_out=scores, keep_out=keep)
+    _check_evict(cache, before, [C], [N], "l2", scores, keep, pos)
+    vd.vd_evict_step_mx4(twin, [C], [N])
+    assert all(torch.equal(a, b) for a, b in zip(twin, cache))
+
+
+def test_evict_survives_nan_groups():
+    """Rankings are unspecified, but exactly N slots stay and rows stay whole."""
+    n, N, D = 500, 300, 128
+    for one in (False, True):
+        budget = n - 1 if one else N
+        cache = _cache(1, 1, 2, n, D, 99)
+        cache.v_scale[0, 0, 0, ::3] = 255
+        before = [x.cpu().clone() for x in cache]
+        keep = torch.zeros((2, n), dtype=torch.uint8, device=DEV)
+        vd.vd_evict_step_mx4(cache, [n], [budget], keep_out=keep)
+        assert keep.sum(1).tolist() == [budget, budget]
+        for h in range(2):
+            stay = keep[h].nonzero().flatten().tolist()
+            slots = torch.arange(n)
+            for a, b in ref.moves(stay, n, budget):
+                slots[b] = a
+            for x, y in zip(cache, before):
+                assert torch.equal(x[0, 0, h].cpu(), y[0, 0, h, slots])
+
+
+# ------------------------------------------------------------------ together
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_block_processing_and_decode(dtype):
+    """Prompt blocks (the last one partial), then decode steps: norm and rotation,
+    append, attend, evict, each against the definitions on the state before it."""
+    S, L, H, G, D, N, B = 2, 2, 2, 3, 64, 48, 20
+    cache = Mx4EvictingCache(S, L, H, D, N + B, [N, N - 7], device=DEV)
+    inv_freq = (10000.0 ** (-torch.arange(0, D, 2).double() / D)).float().to(DEV)
+    w = (1 + 0.1 * torch.randn(L, D, generator=torch.Generator().manual_seed(3))).to(DEV)
+    for step, rows in enumerate([[B, B], [B, B], [B, 9], [B, 1], [1, 1], [1, 1], [1, 0]]):
+        t = max(rows)
+        q = _rows((S, L, H * G, t, D), dtype, 100 + step, 0.3).to(DEV)
+        k = _rows((S, L, H, t, D), dtype, 200 + step, 0.3).to(DEV)
+        v = _rows((S, L, H, t, D), dtype, 300 + step).to(DEV)
+        pos = (torch.tensor(cache.seen).view(S, 1) + torch.arange(t)).int().to(DEV)
+        q, k = vd.vd_qk_norm_rope(q, k, pos, inv_freq, w, w, q, k)      # in place
+        before = [x.cpu().clone() for x in cache.cache]
+        n_old, seen = list(cache.n), list(cache.seen)
+        cache.append(k, v, rows)
+        for i, x in ((0, k), (1, v)):
+            codes, scales = ref.encode(x)
+            for s in range(S):
+                before[i][s, :, :, n_old[s]:cache.n[s]] = codes[s, :, :, :rows[s]]
+                before[2 + i][s, :, :, n_old[s]:cache.n[s]] = scales[s, :, :, :rows[s]]
+        assert all(torch.equal(x.cpu(), y) for x, y in zip(cache.cache, before))
+        out = cache.attend(q, rows)
+        _check_attention(cache.cache, q, cache.n, rows, out, D ** -0.5)
+        C, n = cache.capacity, list(cache.n)
+        scores, keep = torch.full((cache.units, C), -9.0, device=DEV), torch.full((cache.units, C), 7, dtype=torch.uint8, device=DEV)
+        old_pos = cache.pos.cpu().view(S, L, H, C).clone()
+        assert all(old_pos[s, :, :, n_old[s]:n[s]].eq(torch.arange(seen[s], seen[s] + rows[s])).all() for s in range(S))
+        slots = torch.arange(C, dtype=torch.int32, device=DEV).repeat(cache.units, 1)
+        kept_pos, cache.pos = cache.pos, slots           # the slots themselves, to check the moves
+        cache.evict(scores, keep)
+        _check_evict(cache.cache, before, n, cache.budget, "l2", scores, keep, slots)
+        cache.pos = torch.gather(kept_pos, 1, slots.long())
+        assert cache.n == [min(a, b) for a, b in zip(n, cache.budget)]
+
+
+def test_graph_replays():
+    """A decode step in a graph, with its workspace from the graph's pool: every
+    replay against the eager calls, eager work between them."""
+    S, L, H, G, D, N = 2, 1, 2, 4, 128, 2000
+    a, b = [Mx4EvictingCache(S, L, H, D, N + 1, [N] * S, device=DEV) for _ in range(2)]
+    fill = [_rows((S, L, H, N, D), torch.bfloat16, 400 + i).to(DEV) for i in (0, 1)]
+    for c in (a, b):
+        c.append(*fill)
+    q, k, v = (torch.zeros((S, L, x, 1, D), dtype=torch.bfloat16, device=DEV) for x in (H * G, H, H))
+
+    def step(c):
+        c.n, c.seen = [N] * S, [N] * S
+        c.append(k, v)
+        out = c.attend(q)
+        c.evict()
+        return out
+
+    assert vd.vd_attention_mx4_workspace_size(a.cache, H * G, 1) > 0
+    saved = [x.clone() for x in (*a.cache, a.pos)]
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        step(a)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        captured = step(a)
+    for x, y in zip((*a.cache, a.pos), saved):
+        x.copy_(y)
+    for r in range(4):
+        q.copy_(_rows(q.shape, torch.bfloat16, 500 + r, 0.3))
+        k.copy_(_rows(k.shape, torch.bfloat16, 510 + r))
+        v.copy_(_rows(v.shape, torch.bfloat16, 520 + r))
+        graph.replay()
+        torch.cuda.synchronize()
+        want = step(b)
+        torch.cuda.synchronize()
+        assert torch.equal(captured, want)
+        assert all(torch.equal(x, y) for x, y in zip((*a.cache, a.pos), (*b.cache, b.pos)))
+
+
+def test_other_streams():
+    """Calls on a stream of their own: the outputs they allocate belong to it."""
+    cache = _cache(1, 1, 2, 5000, 128, 111)
+    q = _rows((1, 1, 8, 1, 128), torch.bfloat16, 112, 0.3).to(DEV)
+    want = vd.vd_attention_mx4(cache, q, [5000])
+    torch.cuda.synchronize()
+    stream = torch.cuda.Stream()
+    outs = [vd.vd_attention_mx4(cache, q, [5000], stream=stream) for _ in range(5)]
+    ext = torch.cuda.ExternalStream(stream.cuda_stream)
+    outs.append(vd.vd_attention_mx4(cache, q, [5000], stream=ext))
+    rows = vd.vd_read_mx4(cache, [0], 10, stream=stream)
+    stream.synchronize()
+    assert all(torch.equal(x, want) for x in outs)
+    assert torch.equal(rows[0].cpu().double(), ref.decode(cache.k, cache.k_scale)[:, :, :, :10])
