@@ -448,22 +448,60 @@ __global__ __launch_bounds__(kMxThreads) void attn_join_kernel(const MxAttnParam
 // the mean, the N highest, the gather.  Values are exact, sums and distances fp64:
 // the fp32 scores, which the selection ranks, are correctly rounded but for a
 // last-bit tie, whatever the order of the sums.
+//
+// A lane takes one group of a row (16 bytes and a scale), and always the same
+// channels, whose sums and then means stay in its registers.  What bounds it is the
+// conversion of each value to fp64 and one or two operations on it there, twice
+// (17 bytes of memory a lane's row), not the reads.
 
 constexpr int kEvictWaves = kMxEvictThreads / 64;
+constexpr int kEvictBatch = 4;    // rows of a lane in flight
+constexpr int kEvictBins = 2 * kMxEvictThreads;
 
 struct EvictHead {
-    uint32_t hist[256];
-    uint32_t word[8];               // broadcast
+    uint32_t hist[kEvictBins];
+    uint32_t low[kEvictWaves], high[kEvictWaves];   // smallest and largest key
     uint32_t count[2][kEvictWaves];
-    unsigned long long low[kEvictWaves];
+    uint32_t word[4];
+    uint32_t cand_key[64], cand_slot[64];
     double mean[256];
     double len[1];
 };
 
+template <int CTRL>
+__device__ __forceinline__ double dpp_double(double x) {
+    const unsigned long long b = __builtin_bit_cast(unsigned long long, x);
+    const uint32_t lo = dpp<CTRL>(uint32_t(b)), hi = dpp<CTRL>(uint32_t(b >> 32));
+    return __builtin_bit_cast(double, (unsigned long long)(hi) << 32 | lo);
+}
 __device__ __forceinline__ double shfl_xor_double(double x, int d) {
     const unsigned long long b = __builtin_bit_cast(unsigned long long, x);
     const uint32_t lo = __shfl_xor(uint32_t(b), d), hi = __shfl_xor(uint32_t(b >> 32), d);
     return __builtin_bit_cast(double, (unsigned long long)(hi) << 32 | lo);
+}
+// Sum over the LANES neighbouring lanes (2, 4 or 8) of a row, in each of them.
+template <int LANES>
+__device__ __forceinline__ double row_sum(double x) {
+    x += dpp_double<kXor1>(x);
+    if (LANES >= 4) x += dpp_double<kXor2>(x);
+    if (LANES >= 8) x += dpp_double<0x141>(x);   // the other four of eight
+    return x;
+}
+// In lanes [0, 32) the sum of a over both halves of the wave, in [32, 64) that of b
+// (Upper false: over both sixteens of each half).
+template <bool UPPER>
+__device__ __forceinline__ double halves_sum(double a, double b) {
+    const unsigned long long x = __builtin_bit_cast(unsigned long long, a), y = __builtin_bit_cast(unsigned long long, b);
+    u32x2 lo, hi;
+    if (UPPER) {
+        lo = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane32_swap(uint32_t(x), uint32_t(y), false, false));
+        hi = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane32_swap(uint32_t(x >> 32), uint32_t(y >> 32), false, false));
+    } else {
+        lo = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane16_swap(uint32_t(x), uint32_t(y), false, false));
+        hi = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane16_swap(uint32_t(x >> 32), uint32_t(y >> 32), false, false));
+    }
+    return __builtin_bit_cast(double, (unsigned long long)(hi[0]) << 32 | lo[0]) +
+           __builtin_bit_cast(double, (unsigned long long)(hi[1]) << 32 | lo[1]);
 }
 
 // A larger key ranks higher; KeyNorm keeps the smallest norms.
@@ -473,7 +511,126 @@ __device__ __forceinline__ uint32_t rank_key(float score, bool smallest) {
     return smallest ? ~b : b;
 }
 
-template <int D>
+struct GroupRow {
+    u32x4 x;
+    uint32_t scale;
+};
+// A lane's groups of the rows j, j + step, ...; rows behind the last read as 0.
+__device__ __forceinline__ void load_groups(GroupRow (&r)[kEvictBatch], const char *xb, const char *sb, uint32_t slot,
+                                            uint32_t sslot, int g, int j, int step, int n) {
+#pragma unroll
+    for (int u = 0; u < kEvictBatch; ++u) {
+        const int row = j + u * step;
+        const uint32_t at = uint32_t(min(row, n - 1));
+        r[u].x = reinterpret_cast<const u32x4 *>(xb + at * slot)[g];
+        r[u].scale = uint8_t(sb[at * sslot + g]);
+        if (row >= n) r[u].x = u32x4{0, 0, 0, 0}, r[u].scale = 0;
+    }
+}
+// Calls f(channel, value) for the 32 values of a group.
+template <class F>
+__device__ __forceinline__ void each_value(const GroupRow &r, F f) {
+    const float scale = scale_of(r.scale);
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+        const f32x2 a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(r.x[w], scale, 0);
+        const f32x2 b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(r.x[w], scale, 1);
+        const f32x2 c = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(r.x[w], scale, 2);
+        const f32x2 d = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(r.x[w], scale, 3);
+        f(8 * w + 0, double(a[0])), f(8 * w + 1, double(a[1])), f(8 * w + 2, double(b[0])), f(8 * w + 3, double(b[1]));
+        f(8 * w + 4, double(c[0])), f(8 * w + 5, double(c[1])), f(8 * w + 6, double(d[0])), f(8 * w + 7, double(d[1]));
+    }
+}
+
+// The boundary of the N highest of n > N keys (equal ones by the lower slot): a
+// row stays if its key is above `key`, or equal to it in a slot up to `slot`.
+// Keys are counted in bins of equal width between the smallest and the largest; the
+// bin that the boundary falls into is narrowed until it holds at most 64 keys,
+// which one wave ranks, or one value.
+struct Boundary {
+    uint32_t key;
+    int slot;
+};
+__device__ __forceinline__ Boundary boundary(EvictHead &sh, const uint32_t *keys, int n, int N, uint32_t low, uint32_t high) {
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    int want = N;   // keys to keep among those in [low, high]
+    for (;;) {
+        const uint32_t range = high - low;
+        const int shift = range < uint32_t(kEvictBins) ? 0 : 32 - __builtin_clz(range) - 11;   // (2^11 bins)
+        for (int i = tid; i < kEvictBins; i += kMxEvictThreads) sh.hist[i] = 0;
+        __syncthreads();
+        for (int j = tid; j < n; j += kMxEvictThreads) {
+            const uint32_t at = keys[j] - low;
+            if (at <= range) atomicAdd(&sh.hist[at >> shift], 1u);
+        }
+        __syncthreads();
+        // from the highest bin down, two bins a thread
+        const uint32_t c0 = sh.hist[kEvictBins - 1 - 2 * tid], c1 = sh.hist[kEvictBins - 2 - 2 * tid];
+        uint32_t upto = c0 + c1;
+        for (int d = 1; d < 64; d *= 2) {
+            const uint32_t o = __shfl_up(upto, d);
+            if (lane >= d) upto += o;
+        }
+        if (lane == 63) sh.count[0][wave] = upto;
+        __syncthreads();
+        for (int w = 0; w < kEvictWaves; ++w) upto += w < wave ? sh.count[0][w] : 0u;
+        const uint32_t before = upto - c0 - c1;
+        if (before < uint32_t(want) && before + c0 >= uint32_t(want)) {
+            sh.word[0] = uint32_t(kEvictBins - 1 - 2 * tid), sh.word[1] = before, sh.word[2] = c0;
+        } else if (before + c0 < uint32_t(want) && upto >= uint32_t(want)) {
+            sh.word[0] = uint32_t(kEvictBins - 2 - 2 * tid), sh.word[1] = before + c0, sh.word[2] = c1;
+        }
+        if (tid == 0) sh.word[3] = 0;
+        __syncthreads();
+        const uint32_t bin = sh.word[0], count = sh.word[2];
+        want -= int(sh.word[1]);
+        low += bin << shift;
+        high = min(high, low + ((1u << shift) - 1));
+        if (count <= 64) {
+            for (int j = tid; j < n; j += kMxEvictThreads) {
+                const uint32_t key = keys[j];
+                if (key - low <= high - low) {
+                    const uint32_t i = atomicAdd(&sh.word[3], 1u);
+                    if (i < 64) sh.cand_key[i] = key, sh.cand_slot[i] = uint32_t(j);
+                }
+            }
+            __syncthreads();
+            if (wave == 0) {
+                const bool mine = lane < int(count);
+                const uint32_t key = mine ? sh.cand_key[lane] : 0u, slot = mine ? sh.cand_slot[lane] : 0u;
+                int rank = 0;
+                for (int i = 0; i < int(count); ++i) {
+                    const uint32_t k = __shfl(key, i), s = __shfl(slot, i);
+                    rank += k > key || (k == key && s < slot);
+                }
+                if (mine && rank == want - 1) sh.word[0] = key, sh.word[1] = slot;
+            }
+            __syncthreads();
+            return {sh.word[0], int(sh.word[1])};
+        }
+        if (shift == 0) break;
+    }
+    // more than 64 equal keys: the slot of the want-th of them; a wave takes a run of slots
+    const int span = (n + kMxEvictThreads - 1) / kMxEvictThreads * 64;
+    const int first = wave * span, last = min(first + span, n);
+    int ties = 0;
+    for (int base = first; base < last; base += 64)
+        ties += __popcll(__builtin_amdgcn_ballot_w64(base + lane < last && keys[min(base + lane, n - 1)] == low));
+    if (lane == 0) sh.count[0][wave] = uint32_t(ties);
+    __syncthreads();
+    int before = 0;
+    for (int w = 0; w < kEvictWaves; ++w) before += w < wave ? int(sh.count[0][w]) : 0;
+    for (int base = first; base < last; base += 64) {
+        const bool tie = base + lane < last && keys[min(base + lane, n - 1)] == low;
+        const unsigned long long b = __builtin_amdgcn_ballot_w64(tie);
+        if (tie && before + __popcll(b & ((1ull << lane) - 1)) == want - 1) sh.word[1] = uint32_t(base + lane);
+        before += __popcll(b);
+    }
+    __syncthreads();
+    return {low, int(sh.word[1])};
+}
+
+template <int D, int FORM>
 __global__ __launch_bounds__(kMxEvictThreads) void evict_kernel(const MxEvictParams p) {
     constexpr int LANES = D / 32;                         // lanes of a row: a group each
     constexpr int ROWS = kMxEvictThreads / LANES;         // rows that the workgroup takes at a time
@@ -490,42 +647,40 @@ __global__ __launch_bounds__(kMxEvictThreads) void evict_kernel(const MxEvictPar
     const int64_t code_at = s * p.c.seq + layer * p.c.layer + head * p.c.head;
     const int64_t scale_at = s * p.c.sseq + layer * p.c.slayer + head * p.c.shead;
     const bool key_side = p.variant >= VD_SCORE_KEY_L2;
-    const int form = p.variant - (key_side ? VD_SCORE_KEY_L2 : 0);   // L2, Dir, Norm
     const bool smallest = p.variant == VD_SCORE_KEY_NORM;
     float *scores = p.scores ? p.scores + unit * p.capacity : nullptr;
     uint8_t *keep = p.keep ? p.keep + unit * p.capacity : nullptr;
-    if (n <= N && !scores) {
-        if (keep)
-            for (int j = tid; j < n; j += kMxEvictThreads) keep[j] = 1;
-        return;
-    }
+    if (n <= N && keep)
+        for (int j = tid; j < n; j += kMxEvictThreads) keep[j] = 1;
+    if (n <= N && !scores) return;
     const char *xb = (key_side ? p.c.k : p.c.v) + code_at, *sb = (key_side ? p.c.ks : p.c.vs) + scale_at;
     const int g = tid % LANES, r0 = tid / LANES;
 
+    GroupRow row[kEvictBatch];
     double mean[32];
 #pragma unroll
     for (int i = 0; i < 32; ++i) mean[i] = 0.0;
-    if (form != VD_SCORE_NORM) {
-        for (int j = r0; j < n; j += ROWS) {
-            const u32x4 x = reinterpret_cast<const u32x4 *>(xb + uint32_t(j) * p.c.slot)[g];
-            const float scale = scale_of(uint8_t(sb[uint32_t(j) * p.c.sslot + g]));
+    double length = 0.0;
+    if (FORM != VD_SCORE_NORM) {
+        for (int j = r0; j < n; j += kEvictBatch * ROWS) {
+            load_groups(row, xb, sb, p.c.slot, p.c.sslot, g, j, ROWS, n);
 #pragma unroll
-            for (int w = 0; w < 4; ++w) {
-                const f32x2 a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(x[w], scale, 0);
-                const f32x2 b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(x[w], scale, 1);
-                const f32x2 c = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(x[w], scale, 2);
-                const f32x2 d = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(x[w], scale, 3);
-                mean[8 * w + 0] += double(a[0]), mean[8 * w + 1] += double(a[1]);
-                mean[8 * w + 2] += double(b[0]), mean[8 * w + 3] += double(b[1]);
-                mean[8 * w + 4] += double(c[0]), mean[8 * w + 5] += double(c[1]);
-                mean[8 * w + 6] += double(d[0]), mean[8 * w + 7] += double(d[1]);
+            for (int u = 0; u < kEvictBatch; ++u) {
+                each_value(row[u], [&](int i, double v) { mean[i] += v; });
+                __builtin_amdgcn_sched_barrier(0);   // one row's conversions at a time: registers
             }
         }
+        // over the lanes with the same group: halves of the wave and of those keep half
+        // of the channels each, then the lanes of sixteen are added up
 #pragma unroll
-        for (int i = 0; i < 32; ++i) {
+        for (int i = 0; i < 16; ++i) mean[i] = halves_sum<true>(mean[i], mean[i + 16]);
 #pragma unroll
-            for (int d = LANES; d < 64; d *= 2) mean[i] += shfl_xor_double(mean[i], d);
-            if (lane < LANES) partial[wave * D + lane * 32 + i] = mean[i];
+        for (int i = 0; i < 8; ++i) {
+            double t = halves_sum<false>(mean[i], mean[i + 8]);
+            if (LANES <= 8) t += dpp_double<0x128>(t);   // row_ror:8
+            if (LANES <= 4) t += dpp_double<0x124>(t);   // row_ror:4
+            if (LANES <= 2) t += dpp_double<0x122>(t);   // row_ror:2
+            if ((lane & 15) < LANES) partial[wave * D + g * 32 + i + 8 * ((lane >> 4) & 1) + 16 * (lane >> 5)] = t;
         }
         __syncthreads();
         if (tid < D) {
@@ -534,146 +689,120 @@ __global__ __launch_bounds__(kMxEvictThreads) void evict_kernel(const MxEvictPar
             sh.mean[tid] = t / double(n);
         }
         __syncthreads();
-        if (form == VD_SCORE_DIR && wave == 0) {
-            double t = 0.0;
-            for (int c = lane; c < D; c += 64) t = fma(sh.mean[c], sh.mean[c], t);
-            for (int d = 1; d < 64; d *= 2) t += shfl_xor_double(t, d);
-            if (lane == 0) sh.len[0] = sqrt(t);
+        if (FORM == VD_SCORE_DIR) {
+            if (wave == 0) {
+                double t = 0.0;
+                for (int c = lane; c < D; c += 64) t = fma(sh.mean[c], sh.mean[c], t);
+                for (int d = 1; d < 64; d *= 2) t += shfl_xor_double(t, d);
+                if (lane == 0) sh.len[0] = sqrt(t);
+            }
+            __syncthreads();
+            length = sh.len[0];
         }
-        __syncthreads();
 #pragma unroll
         for (int i = 0; i < 32; ++i) mean[i] = sh.mean[g * 32 + i];
     }
-    const double length = form == VD_SCORE_DIR ? sh.len[0] : 0.0;
 
-    for (int j = r0; j < n; j += ROWS) {
-        const u32x4 x = reinterpret_cast<const u32x4 *>(xb + uint32_t(j) * p.c.slot)[g];
-        const float scale = scale_of(uint8_t(sb[uint32_t(j) * p.c.sslot + g]));
-        double sq = 0.0, dot = 0.0;
+    uint32_t low = ~0u, high = 0u;
+    for (int j = r0; j < n; j += kEvictBatch * ROWS) {
+        load_groups(row, xb, sb, p.c.slot, p.c.sslot, g, j, ROWS, n);
+        double sq[kEvictBatch], dot[kEvictBatch];
 #pragma unroll
-        for (int w = 0; w < 4; ++w) {
-            const f32x2 y[4] = {__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(x[w], scale, 0), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(x[w], scale, 1),
-                                __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(x[w], scale, 2), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(x[w], scale, 3)};
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const double v = double(y[e >> 1][e & 1]), m = mean[8 * w + e];
-                if (form == VD_SCORE_DIR) {
-                    sq = fma(v, v, sq);
-                    dot = fma(v, m, dot);
-                } else {
-                    sq = fma(v - m, v - m, sq);   // (Norm: m is 0)
-                }
-            }
+        for (int u = 0; u < kEvictBatch; ++u) {
+            double a = 0.0, b = 0.0;
+            each_value(row[u], [&](int i, double v) {
+                if (FORM == VD_SCORE_L2) v -= mean[i];
+                a = fma(v, v, a);
+                if (FORM == VD_SCORE_DIR) b = fma(v, mean[i], b);
+            });
+            sq[u] = row_sum<LANES>(a);
+            if (FORM == VD_SCORE_DIR) dot[u] = row_sum<LANES>(b);
+            __builtin_amdgcn_sched_barrier(0);
         }
+        // every lane of a row has its sums: the row's lanes finish one row of the batch each
 #pragma unroll
-        for (int d = 1; d < LANES; d *= 2) sq += shfl_xor_double(sq, d), dot += shfl_xor_double(dot, d);
-        if (g == 0) {
-            double score = sqrt(sq);
-            if (form == VD_SCORE_DIR) {
+        for (int u0 = 0; u0 < kEvictBatch; u0 += LANES) {
+            const int u = u0 + g;
+            double a = sq[u0], b = FORM == VD_SCORE_DIR ? dot[u0] : 0.0;
+#pragma unroll
+            for (int e = 1; e < (LANES < kEvictBatch ? LANES : kEvictBatch); ++e) {
+                a = g == e ? sq[(u0 + e) % kEvictBatch] : a;
+                if (FORM == VD_SCORE_DIR) b = g == e ? dot[(u0 + e) % kEvictBatch] : b;
+            }
+            double score = sqrt(a);
+            if (FORM == VD_SCORE_DIR) {
                 const double both = score * length;
-                score = both > 0.0 ? 1.0 - dot / both : both == 0.0 ? 1.0 : both;
+                score = both > 0.0 ? 1.0 - b / both : both == 0.0 ? 1.0 : both;
             }
-            const float out = float(score);
-            if (scores) scores[j] = out;
-            if (n > N) keys[j] = rank_key(out, smallest);
+            const int slot = j + u * ROWS;
+            if (u < kEvictBatch && slot < n) {
+                const float out = float(score);
+                const uint32_t key = rank_key(out, smallest);
+                low = min(low, key);
+                high = max(high, key);
+                if (scores) scores[slot] = out;
+                if (n > N) keys[slot] = key;
+            }
         }
     }
-    if (n <= N) {
-        if (keep)
-            for (int j = tid; j < n; j += kMxEvictThreads) keep[j] = 1;
-        return;
-    }
+    if (n <= N) return;
+    for (int d = 1; d < 64; d *= 2) low = min(low, __shfl_xor(low, d)), high = max(high, __shfl_xor(high, d));
+    if (lane == 0) sh.low[wave] = low, sh.high[wave] = high;
     __syncthreads();
+    for (int w = 0; w < kEvictWaves; ++w) low = min(low, sh.low[w]), high = max(high, sh.high[w]);
 
     int moved;   // rows to move: movers[k] onto holes[k]
     if (n == N + 1) {
         // the lowest key goes, the highest slot among equal ones
-        unsigned long long low = ~0ull;
-        for (int j = tid; j < n; j += kMxEvictThreads) {
-            const unsigned long long at = (unsigned long long)(keys[j]) << 32 | uint32_t(~j);
-            low = at < low ? at : low;
-        }
-        for (int d = 1; d < 64; d *= 2) {
-            const uint32_t a = __shfl_xor(uint32_t(low), d), b = __shfl_xor(uint32_t(low >> 32), d);
-            const unsigned long long o = (unsigned long long)(b) << 32 | a;
-            low = o < low ? o : low;
-        }
-        if (lane == 0) sh.low[wave] = low;
+        int gone = -1;
+        for (int j = tid; j < n; j += kMxEvictThreads)
+            if (keys[j] == low) gone = j;
+        for (int d = 1; d < 64; d *= 2) gone = max(gone, __shfl_xor(gone, d));
+        if (lane == 0) sh.count[0][wave] = uint32_t(gone + 1);
         __syncthreads();
-        for (int w = 0; w < kEvictWaves; ++w) low = sh.low[w] < low ? sh.low[w] : low;
-        const int gone = int(~uint32_t(low));
+        for (int w = 0; w < kEvictWaves; ++w) gone = max(gone, int(sh.count[0][w]) - 1);
         if (keep)
             for (int j = tid; j < n; j += kMxEvictThreads) keep[j] = j != gone;
         if (tid == 0) holes[0] = uint16_t(gone), movers[0] = uint16_t(N);
         moved = gone < N;
         __syncthreads();
     } else {
-        // the N-th highest key by its bytes, highest first
-        uint32_t prefix = 0;
-        int want = N;   // rows still to find among those that share the prefix
-        for (int shift = 24; shift >= 0; shift -= 8) {
-            if (tid < 256) sh.hist[tid] = 0;
-            __syncthreads();
-            for (int j = tid; j < n; j += kMxEvictThreads) {
-                const uint32_t key = keys[j];
-                if (shift == 24 || (key >> (shift + 8)) == (prefix >> (shift + 8))) atomicAdd(&sh.hist[(key >> shift) & 255u], 1u);
-            }
-            __syncthreads();
-            if (wave == 0) {   // lane: bins 255 - 4 lane downwards
-                uint32_t c[4], sum = 0;
-                for (int i = 0; i < 4; ++i) sum += c[i] = sh.hist[255 - 4 * lane - i];
-                uint32_t upto = sum;
-                for (int d = 1; d < 64; d *= 2) {
-                    const uint32_t o = __shfl_up(upto, d);
-                    if (lane >= d) upto += o;
-                }
-                uint32_t before = upto - sum;
-                for (int i = 0; i < 4; ++i) {
-                    if (before < uint32_t(want) && before + c[i] >= uint32_t(want)) {
-                        sh.word[0] = uint32_t(255 - 4 * lane - i);
-                        sh.word[1] = before;
-                    }
-                    before += c[i];
-                }
-            }
-            __syncthreads();
-            prefix |= sh.word[0] << shift;
-            want -= int(sh.word[1]);
-        }
-        // keys above `prefix` stay, and of those equal to it the first `want`
-        int ties = 0, nh = 0, nm = 0;   // so far
+        const Boundary edge = boundary(sh, keys, n, N, low, high);
+        // the lists in the order of the slots: a wave takes a run of them, counts, then writes
+        const int span = (n + kMxEvictThreads - 1) / kMxEvictThreads * 64;
+        const int first = wave * span, last = min(first + span, n);
         const unsigned long long below = (1ull << lane) - 1;
-        for (int base = 0; base < n; base += kMxEvictThreads) {
-            const int j = base + tid;
-            const uint32_t key = j < n ? keys[j] : 0u;
-            const bool tie = j < n && key == prefix;
-            const unsigned long long tb = __builtin_amdgcn_ballot_w64(tie);
-            if (lane == 0) sh.count[0][wave] = __popcll(tb);
-            __syncthreads();
-            int tie_rank = ties + __popcll(tb & below);
-            for (int w = 0; w < kEvictWaves; ++w) {
-                tie_rank += w < wave ? int(sh.count[0][w]) : 0;
-                ties += int(sh.count[0][w]);
-            }
-            __syncthreads();
-            const bool kept = j < n && (key > prefix || (tie && tie_rank < want));
-            if (keep && j < n) keep[j] = kept;
-            const bool hole = j < min(N, n) && !kept, mover = kept && j >= N;
+        auto stays = [&](int j) { return keys[j] > edge.key || (keys[j] == edge.key && j <= edge.slot); };
+        int nh = 0, nm = 0;
+        for (int base = first; base < last; base += 64) {
+            const int j = base + lane;
+            const bool kept = j < last && stays(j);
+            if (keep && j < last) keep[j] = kept;
+            nh += __popcll(__builtin_amdgcn_ballot_w64(j < min(N, last) && !kept));
+            nm += __popcll(__builtin_amdgcn_ballot_w64(j >= N && kept));
+        }
+        if (lane == 0) sh.count[0][wave] = uint32_t(nh), sh.count[1][wave] = uint32_t(nm);
+        __syncthreads();
+        int hr = 0, mr = 0;
+        nh = nm = 0;
+        for (int w = 0; w < kEvictWaves; ++w) {
+            hr += w < wave ? int(sh.count[0][w]) : 0;
+            mr += w < wave ? int(sh.count[1][w]) : 0;
+            nh += int(sh.count[0][w]);
+            nm += int(sh.count[1][w]);
+        }
+        for (int base = first; base < last; base += 64) {
+            const int j = base + lane;
+            const bool kept = j < last && stays(j), hole = j < min(N, last) && !kept, mover = j >= N && kept;
             const unsigned long long hb = __builtin_amdgcn_ballot_w64(hole), mb = __builtin_amdgcn_ballot_w64(mover);
-            if (lane == 0) sh.count[0][wave] = __popcll(hb), sh.count[1][wave] = __popcll(mb);
-            __syncthreads();
-            int hr = nh + __popcll(hb & below), mr = nm + __popcll(mb & below);
-            for (int w = 0; w < kEvictWaves; ++w) {
-                hr += w < wave ? int(sh.count[0][w]) : 0;
-                mr += w < wave ? int(sh.count[1][w]) : 0;
-                nh += int(sh.count[0][w]);
-                nm += int(sh.count[1][w]);
-            }
-            if (hole && hr < p.list_cap) holes[hr] = uint16_t(j);
-            if (mover && mr < p.list_cap) movers[mr] = uint16_t(j);
-            __syncthreads();
+            const int hi = hr + __popcll(hb & below), mi = mr + __popcll(mb & below);
+            if (hole && hi < p.list_cap) holes[hi] = uint16_t(j);
+            if (mover && mi < p.list_cap) movers[mi] = uint16_t(j);
+            hr += __popcll(hb);
+            mr += __popcll(mb);
         }
         moved = min(min(nh, nm), p.list_cap);
+        __syncthreads();
     }
 
     // codes in 16-byte words (K's, then V's), scales in one word of D / 32 bytes
@@ -726,7 +855,11 @@ hipError_t launch_attn(const MxAttnParams &p, int seqs, hipStream_t stream) {
 
 template <int D>
 hipError_t launch_evict(const MxEvictParams &p, int seqs, size_t lds, hipStream_t stream) {
-    return launch_with(evict_kernel<D>, dim3(p.c.heads, p.c.layers, seqs), kMxEvictThreads, lds, stream, p);
+    const int form = p.variant - (p.variant >= VD_SCORE_KEY_L2 ? VD_SCORE_KEY_L2 : 0);
+    return launch_with(form == VD_SCORE_L2    ? evict_kernel<D, VD_SCORE_L2>
+                       : form == VD_SCORE_DIR ? evict_kernel<D, VD_SCORE_DIR>
+                                              : evict_kernel<D, VD_SCORE_NORM>,
+                       dim3(p.c.heads, p.c.layers, seqs), kMxEvictThreads, lds, stream, p);
 }
 
 }  // namespace
