@@ -152,19 +152,20 @@ vd_status rows_call(const vd_mx4_cache *cache, const int32_t *first, const int32
     return VD_OK;
 }
 
-// Tiles of query rows and splits of the cache rows.  A workgroup's four waves
-// take 128 cache rows at a time, about four workgroups stay resident on a CU.
+// Tiles of query rows and splits of the cache rows.
 struct AttnPlan {
-    int tiles, splits;
+    int block, tiles, splits;
 };
-constexpr int kResident = 4 * 256;
-AttnPlan attn_plan(const vd_mx4_cache *c, int64_t max_rows, int64_t n) {
-    const int64_t group = c->num_q_heads / c->num_kv_heads;
+AttnPlan attn_plan(const vd_mx4_cache *c, int32_t dtype, int64_t max_rows, int64_t n) {
+    const int64_t queries = max_rows * (c->num_q_heads / c->num_kv_heads);
     const int64_t units = int64_t(c->num_seqs) * c->num_layers * c->num_kv_heads;
     AttnPlan a;
-    a.tiles = int((max_rows * group + vd::kMxTile - 1) / vd::kMxTile);
-    const int64_t groups = units * a.tiles;
-    a.splits = int(std::max<int64_t>(1, std::min<int64_t>({vd::kMxMaxSplits, kResident / groups, n / 256})));
+    // (three parts of 256 channels of a query do not fit the block kernel's registers)
+    a.block = queries > vd::kMxTile && !(dtype == VD_DTYPE_F32 && c->head_dim == 256);
+    const int64_t tile = a.block ? vd::kMxBlockTile : vd::kMxTile;
+    a.tiles = int((queries + tile - 1) / tile);
+    const int64_t groups = units * a.tiles, resident = (a.block ? 2 : 4) * 256;
+    a.splits = int(std::max<int64_t>(1, std::min<int64_t>({vd::kMxMaxSplits, resident / groups, n / 256})));
     return a;
 }
 // [unit][split][query row]: D sums, then two floats each.
@@ -196,7 +197,7 @@ extern "C" vd_status vd_read_mx4(const vd_mx4_cache *cache, const int32_t *first
 
 extern "C" size_t vd_attention_mx4_workspace_size(const vd_mx4_cache *cache, int32_t dtype, int32_t max_rows, int32_t n) {
     if (check_cache(cache, false) != VD_OK || check_queries(cache, dtype, max_rows) != VD_OK || n < 0 || n > cache->capacity) return 0;
-    return attn_ws(cache, max_rows, attn_plan(cache, max_rows, n));
+    return attn_ws(cache, max_rows, attn_plan(cache, dtype, max_rows, n));
 }
 
 extern "C" vd_status vd_attention_mx4(const vd_mx4_cache *cache, int32_t dtype, const void *q, const int64_t *q_strides,
@@ -222,7 +223,7 @@ extern "C" vd_status vd_attention_mx4(const vd_mx4_cache *cache, int32_t dtype, 
     if (shares(count, p.os, 4) || oe.meets(qe)) return VD_ERR_INVALID_ARG;
     for (const Extent &c : cached)
         if (oe.meets(c)) return VD_ERR_INVALID_ARG;
-    const AttnPlan a = attn_plan(cache, max_rows, n);
+    const AttnPlan a = attn_plan(cache, dtype, max_rows, n);
     const size_t need = attn_ws(cache, max_rows, a);
     if (need && (!workspace || !aligned(workspace, 16) || workspace_bytes < need)) return VD_ERR_WORKSPACE;
     const int64_t L = cache->num_layers, per_seq = L * cache->num_q_heads * max_rows * a.splits;   // partial rows
@@ -232,6 +233,7 @@ extern "C" vd_status vd_attention_mx4(const vd_mx4_cache *cache, int32_t dtype, 
     p.max_rows = max_rows;
     p.splits = a.splits;
     p.tiles = a.tiles;
+    p.block = a.block;
     const int chunk = std::max(1, std::min(vd::kMxSeqs, int(65535 / L)));
     for (int s0 = 0; s0 < cache->num_seqs; s0 += chunk) {
         const int ns = std::min(chunk, cache->num_seqs - s0);

@@ -13,6 +13,7 @@ constexpr int kMxGroup = 32;      // channels that share a scale
 constexpr int kMxThreads = 256;   // threads of an append, read or attention workgroup
 constexpr int kMxEvictThreads = 1024;
 constexpr int kMxTile = 16;       // query rows of the attention kernel's tile
+constexpr int kMxBlockTile = 128; // and of the one for blocks of them
 constexpr int kMxMaxSplits = 64;  // the combining wave holds a split per lane
 
 // A 4-bit cache as the kernels see it: bases of the launch's first sequence,
@@ -46,6 +47,7 @@ struct MxAttnParams {
     float qscale;              // softmax scale times log2(e)
     int32_t group;             // query heads per KV head
     int32_t max_rows, splits, tiles;
+    int32_t block;             // the kernel for blocks of query rows, its tiles of kMxBlockTile
     int32_t n[kMxSeqs], rows[kMxSeqs];
 };
 hipError_t launch_mx_attention(const MxAttnParams &p, int seqs, int dtype, int head_dim, hipStream_t stream);

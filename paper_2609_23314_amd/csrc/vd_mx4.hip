@@ -204,6 +204,25 @@ __device__ __forceinline__ Scales<D> load_scales(const char *row) {
     return r;
 }
 
+// Eight channels of a query row, in parts.
+template <int DTYPE, int QP, int FRAGS>
+__device__ __forceinline__ void load_query(bf16x8 (&q)[QP][FRAGS], int f, const char *row, int ch) {
+    if (DTYPE == VD_DTYPE_BF16) {
+        q[0][f] = *reinterpret_cast<const bf16x8 *>(row + ch * 2);
+        return;
+    }
+    const f32x4 a = *reinterpret_cast<const f32x4 *>(row + ch * 4), b = *reinterpret_cast<const f32x4 *>(row + ch * 4 + 16);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        float x = e < 4 ? a[e & 3] : b[e & 3];
+#pragma unroll
+        for (int part = 0; part < QP; ++part) {
+            q[part][f][e] = __bf16(x);
+            x -= float(q[part][f][e]);
+        }
+    }
+}
+
 // Bytes of one wave's V tile: 32 rows of bf16, 32 bytes apart from a multiple
 // of the banks, so that neither the rows' writes nor the turned reads collide.
 template <int D>
@@ -214,11 +233,6 @@ constexpr int attn_lds() {
     const int tiles = 4 * 32 * kVStride<D>, merge = 4 * kMxTile * (D + 4) * 4 + 4 * kMxTile * 2 * 4;
     return tiles > merge ? tiles : merge;
 }
-
-struct AttnUnit {   // what a workgroup works on
-    int n, rows, queries;        // cached rows, query rows, query rows times heads
-    int begin, end;              // its rows of the cache
-};
 
 template <int DTYPE, int D>
 __global__ __launch_bounds__(kMxThreads) void attn_kernel(const MxAttnParams p) {
@@ -241,28 +255,11 @@ __global__ __launch_bounds__(kMxThreads) void attn_kernel(const MxAttnParams p) 
     const int m = m0 + c, i = min(m, queries - 1) / G, g = min(m, queries - 1) - i * G;
     const int limit = n - rows + 1 + i;
 
-    // queries: the right operand, channels kq * D / 4 + 8 f + e of query c
-    bf16x8 q[QP][FRAGS];
+    bf16x8 q[QP][FRAGS];   // the right operand: channels kq * D / 4 + 8 f + e of query c
     {
         const char *src = p.q + s * p.qs[0] + layer * p.qs[1] + (head * G + g) * p.qs[2] + i * p.qs[3];
 #pragma unroll
-        for (int f = 0; f < FRAGS; ++f) {
-            const int ch = kq * (D / 4) + 8 * f;
-            if (DTYPE == VD_DTYPE_BF16) {
-                q[0][f] = *reinterpret_cast<const bf16x8 *>(src + ch * 2);
-            } else {
-                const f32x4 a = *reinterpret_cast<const f32x4 *>(src + ch * 4), b = *reinterpret_cast<const f32x4 *>(src + ch * 4 + 16);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    float x = e < 4 ? a[e & 3] : b[e & 3];
-#pragma unroll
-                    for (int part = 0; part < QP; ++part) {
-                        q[part][f][e] = __bf16(x);
-                        x -= float(q[part][f][e]);
-                    }
-                }
-            }
-        }
+        for (int f = 0; f < FRAGS; ++f) load_query<DTYPE, QP>(q, f, src, kq * (D / 4) + 8 * f);
     }
 
     const char *kb = p.c.k + s * p.c.seq + layer * p.c.layer + head * p.c.head;
@@ -405,6 +402,221 @@ __global__ __launch_bounds__(kMxThreads) void attn_kernel(const MxAttnParams p) 
             *reinterpret_cast<bf16x4 *>(dst + ch * 2) = b;
         }
     }
+}
+
+// Blocks of query rows.  A workgroup takes 128 query rows of a KV head, a wave 32
+// of them, and passes over the cache 64 rows (32 of D = 256) at a time: the four
+// waves convert a tile of K and V into LDS, while they work on the tile before.
+// With v_mfma_f32_32x32x16_bf16 as above, transposed: a lane holds one query's
+// logits of 16 rows of 32, which are the right operand of the product with V^T.
+
+template <int D>
+constexpr int kBlockRows = D == 256 ? 32 : 64;
+template <int D>
+constexpr int kBlockBytes = 2 * kBlockRows<D> * kVStride<D>;   // K's tile, then V's
+
+// A thread's part of a tile on its way from memory: groups of K, then groups of V
+// (of D = 64 one group of either).
+template <int D>
+struct BlockStage {
+    static constexpr int GROUPS = D / 32, ROWS = kBlockRows<D>, ITEMS = 2 * ROWS * GROUPS / kMxThreads, K_ITEMS = (ITEMS + 1) / 2;
+    u32x4 x[ITEMS];
+    Scales<D> ks[K_ITEMS], vs[K_ITEMS];   // of the whole row, whose NaN groups K's items look for
+    uint32_t vbyte[ITEMS];                // of V's items
+    __device__ __forceinline__ static bool is_v(int i) { return ITEMS == 1 ? int(threadIdx.x) >= ROWS * GROUPS : i >= K_ITEMS; }
+    __device__ __forceinline__ static int at(int i) { return (int(threadIdx.x) + i * kMxThreads) % (ROWS * GROUPS); }
+    __device__ __forceinline__ void load(const char *kb, const char *vb, const char *ksb, const char *vsb, uint32_t slot,
+                                         uint32_t sslot, int j0, int end) {
+#pragma unroll
+        for (int i = 0; i < ITEMS; ++i) {
+            const uint32_t row = uint32_t(min(j0 + at(i) / GROUPS, end - 1));   // behind the end: the last row, hidden later
+            x[i] = reinterpret_cast<const u32x4 *>((is_v(i) ? vb : kb) + row * slot)[at(i) % GROUPS];
+            if (i < K_ITEMS) {
+                ks[i % K_ITEMS] = load_scales<D>(ksb + row * sslot);
+                vs[i % K_ITEMS] = load_scales<D>(vsb + row * sslot);
+            } else {
+                vbyte[i] = uint8_t(vsb[row * sslot + at(i) % GROUPS]);
+            }
+        }
+    }
+    __device__ __forceinline__ void store(char *tile) const {
+#pragma unroll
+        for (int i = 0; i < ITEMS; ++i) {
+            const int row = at(i) / GROUPS, group = at(i) % GROUPS;
+            uint32_t byte;
+            if (is_v(i)) {
+                byte = i < K_ITEMS ? vs[i % K_ITEMS].byte(group) : vbyte[i];
+                byte = byte == 255u ? 0u : byte;
+            } else {
+                byte = ks[i % K_ITEMS].has_nan() || vs[i % K_ITEMS].has_nan() ? 255u : ks[i % K_ITEMS].byte(group);
+            }
+            char *to = tile + (is_v(i) ? ROWS * kVStride<D> : 0) + row * kVStride<D> + group * 64;
+#pragma unroll
+            for (int w = 0; w < 4; ++w) reinterpret_cast<bf16x8 *>(to)[w] = decode8(x[i][w], scale_of(byte));
+        }
+    }
+};
+
+__device__ __forceinline__ float dot2(bf16x2 a, bf16x2 b, float c) { return __builtin_amdgcn_fdot2_f32_bf16(a, b, c, false); }
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+
+template <int DTYPE, int D>
+__global__ __launch_bounds__(kMxThreads, 2) void attn_block_kernel(const MxAttnParams p) {
+    constexpr int FRAGS = D / 16, CT = D / 32, SUBS = kBlockRows<D> / 32;
+    constexpr int QP = DTYPE == VD_DTYPE_F32 ? 3 : 1, PP = DTYPE == VD_DTYPE_F32 ? 2 : 1;
+    __shared__ __attribute__((aligned(16))) char lds[2 * kBlockBytes<D>];
+    const int split = blockIdx.x / p.tiles, tile = blockIdx.x % p.tiles;
+    const int head = blockIdx.y, s = blockIdx.z / p.c.layers, layer = blockIdx.z % p.c.layers;
+    const int n = p.n[s], rows = p.rows[s], G = p.group;
+    const int queries = rows * G, m0 = tile * kMxBlockTile;
+    if (m0 >= queries) return;
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, c = lane & 31, half = lane >> 5;
+    const int seen = max(0, n - rows + 1 + min(m0 + kMxBlockTile - 1, queries - 1) / G);
+    constexpr int T = kBlockRows<D>;
+    const int share = ((seen + p.splits - 1) / p.splits + T - 1) / T * T;
+    const int begin = min(split * share, seen), end = min(begin + share, seen);
+    const int wm0 = m0 + 32 * wave, m = wm0 + c;
+    const int i = min(m, queries - 1) / G, g = min(m, queries - 1) - i * G;
+    const int limit = min(n - rows + 1 + i, end);
+    const int all_see = min(n - rows + 1 + min(wm0, queries - 1) / G, end);            // rows that every query of the wave sees
+    const int wave_end = wm0 < queries ? min(n - rows + 1 + min(wm0 + 31, queries - 1) / G, end) : begin;   // and any of them
+
+    bf16x8 q[QP][FRAGS];   // channels 16 f + 8 half + e of query c
+    {
+        const char *src = p.q + s * p.qs[0] + layer * p.qs[1] + (head * G + g) * p.qs[2] + i * p.qs[3];
+#pragma unroll
+        for (int f = 0; f < FRAGS; ++f) load_query<DTYPE, QP>(q, f, src, 16 * f + 8 * half);
+    }
+    const char *kb = p.c.k + s * p.c.seq + layer * p.c.layer + head * p.c.head;
+    const char *vb = p.c.v + s * p.c.seq + layer * p.c.layer + head * p.c.head;
+    const char *ksb = p.c.ks + s * p.c.sseq + layer * p.c.slayer + head * p.c.shead;
+    const char *vsb = p.c.vs + s * p.c.sseq + layer * p.c.slayer + head * p.c.shead;
+
+    f32x16 acc[CT];
+#pragma unroll
+    for (int t = 0; t < CT; ++t)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) acc[t][r] = 0.0f;
+    float top = -INFINITY, sub = 0.0f, sum = 0.0f;   // (the sum of the lane's rows)
+    const bf16x2 ones = {__bf16(1.0f), __bf16(1.0f)};
+
+    BlockStage<D> stage;
+    if (begin < end) {
+        stage.load(kb, vb, ksb, vsb, p.c.slot, p.c.sslot, begin, end);
+        stage.store(lds);
+    }
+    __syncthreads();
+    int buffer = 0;
+    for (int j0 = begin; j0 < end; j0 += T) {
+        const bool more = j0 + T < end;
+        if (more) stage.load(kb, vb, ksb, vsb, p.c.slot, p.c.sslot, j0 + T, end);
+        const char *kt = lds + buffer * kBlockBytes<D>, *vt = kt + T * kVStride<D>;
+        if (j0 < wave_end) {
+            f32x16 z[SUBS];
+#pragma unroll
+            for (int t = 0; t < SUBS; ++t) {
+#pragma unroll
+                for (int r = 0; r < 16; ++r) z[t][r] = 0.0f;
+#pragma unroll
+                for (int f = 0; f < FRAGS; ++f) {
+                    const bf16x8 a = *reinterpret_cast<const bf16x8 *>(kt + (32 * t + c) * kVStride<D> + (16 * f + 8 * half) * 2);
+#pragma unroll
+                    for (int part = QP - 1; part >= 0; --part)
+                        z[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, q[part][f], z[t], 0, 0, 0);
+                }
+            }
+            // lane: query c, rows j0 + 32 t + 8 (r / 4) + 4 half + r % 4
+            float best = -INFINITY;
+            if (j0 + T > all_see) {
+#pragma unroll
+                for (int t = 0; t < SUBS; ++t)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) {
+                        const int j = j0 + 32 * t + 8 * (r >> 2) + 4 * half + (r & 3);
+                        z[t][r] = j < limit ? z[t][r] * p.qscale : -INFINITY;
+                        best = fmaxf(best, z[t][r]);
+                    }
+            } else {
+#pragma unroll
+                for (int t = 0; t < SUBS; ++t)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) {
+                        z[t][r] *= p.qscale;
+                        best = fmaxf(best, z[t][r]);
+                    }
+            }
+            if (__builtin_amdgcn_ballot_w64(best > top + 8.0f)) {   // (as above)
+                best = fmaxf(best, __shfl_xor(best, 32));
+                const float next = fmaxf(top, best);
+                const float to = next == -INFINITY ? 0.0f : next;
+                const float down = __builtin_amdgcn_exp2f(top - to);
+                top = next;
+                sub = to;
+                sum *= down;
+#pragma unroll
+                for (int t = 0; t < CT; ++t)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) acc[t][r] *= down;
+            }
+#pragma unroll
+            for (int t = 0; t < SUBS; ++t)
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {   // sixteen rows
+                    bf16x8 w[PP];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        float x = __builtin_amdgcn_exp2f(z[t][8 * k + e] - sub);
+#pragma unroll
+                        for (int part = 0; part < PP; ++part) {
+                            w[part][e] = __bf16(x);
+                            x -= float(w[part][e]);
+                        }
+                    }
+#pragma unroll
+                    for (int part = 0; part < PP; ++part) {
+                        sum = dot2(__builtin_shufflevector(w[part], w[part], 0, 1), ones, sum);
+                        sum = dot2(__builtin_shufflevector(w[part], w[part], 2, 3), ones, sum);
+                        sum = dot2(__builtin_shufflevector(w[part], w[part], 4, 5), ones, sum);
+                        sum = dot2(__builtin_shufflevector(w[part], w[part], 6, 7), ones, sum);
+                    }
+#pragma unroll
+                    for (int ct = 0; ct < CT; ++ct) {
+                        typedef __attribute__((address_space(3))) s16x4 *lds4;
+                        const char *at = vt + (32 * t + 16 * k + 4 * half + ((lane & 15) >> 2)) * kVStride<D> + ct * 64 +
+                                         ((lane >> 4) & 1) * 32 + (lane & 3) * 8;
+                        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(at));
+                        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(at + 8 * kVStride<D>));
+                        const bf16x8 a = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+#pragma unroll
+                        for (int part = PP - 1; part >= 0; --part)
+                            acc[ct] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, w[part], acc[ct], 0, 0, 0);
+                    }
+                }
+        }
+        buffer ^= 1;
+        if (more) stage.store(lds + buffer * kBlockBytes<D>);
+        __syncthreads();
+    }
+    if (m >= queries) return;
+    sum += __shfl_xor(sum, 32);
+    const int64_t unit = (int64_t(s) * p.c.layers + layer) * p.c.heads + head;
+    const int64_t to = (unit * p.splits + split) * (int64_t(p.max_rows) * G) + m;
+    const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;     // no row seen: 0
+    char *dst = p.out + s * p.os[0] + layer * p.os[1] + (head * G + g) * p.os[2] + i * p.os[3];
+    if (p.splits > 1 && half == 0) p.ws_ml[to * 2] = top, p.ws_ml[to * 2 + 1] = sum;
+#pragma unroll
+    for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+        for (int r = 0; r < 16; r += 4) {
+            const int ch = 32 * ct + 2 * r + 4 * half;
+            const f32x4 x = {acc[ct][r], acc[ct][r + 1], acc[ct][r + 2], acc[ct][r + 3]};
+            if (p.splits > 1)
+                *reinterpret_cast<f32x4 *>(p.ws_acc + to * D + ch) = x;
+            else if (DTYPE == VD_DTYPE_F32)
+                *reinterpret_cast<f32x4 *>(dst + ch * 4) = x * inv;
+            else
+                *reinterpret_cast<bf16x4 *>(dst + ch * 2) = bf16x4{__bf16(x[0] * inv), __bf16(x[1] * inv), __bf16(x[2] * inv), __bf16(x[3] * inv)};
+        }
 }
 
 // Joins the splits of a query row: a wave a row, a lane D / 64 channels.
@@ -846,7 +1058,8 @@ hipError_t launch_rows(const P &p, int seqs, int head_dim, F kernel, hipStream_t
 template <int DTYPE, int D>
 hipError_t launch_attn(const MxAttnParams &p, int seqs, hipStream_t stream) {
     const dim3 grid(uint32_t(p.splits) * p.tiles, p.c.heads, seqs * p.c.layers);
-    const hipError_t e = launch_with(attn_kernel<DTYPE, D>, grid, kMxThreads, 0, stream, p);
+    constexpr bool BLOCK = !(DTYPE == VD_DTYPE_F32 && D == 256);   // (whose registers do not hold it)
+    const hipError_t e = launch_with(p.block ? attn_block_kernel<DTYPE, BLOCK ? D : 128> : attn_kernel<DTYPE, D>, grid, kMxThreads, 0, stream, p);
     if (e != hipSuccess || p.splits == 1) return e;
     const uint32_t per = kMxThreads / 64;
     const dim3 join((uint32_t(p.max_rows) * p.group + per - 1) / per, p.c.heads, seqs * p.c.layers);
