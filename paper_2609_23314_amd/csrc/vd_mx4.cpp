@@ -4,6 +4,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <cfloat>
 #include <cmath>
 #include <cstdint>
 #include <cstring>
@@ -228,7 +229,9 @@ extern "C" vd_status vd_attention_mx4(const vd_mx4_cache *cache, int32_t dtype, 
     if (need && (!workspace || !aligned(workspace, 16) || workspace_bytes < need)) return VD_ERR_WORKSPACE;
     const int64_t L = cache->num_layers, per_seq = L * cache->num_q_heads * max_rows * a.splits;   // partial rows
     const int64_t parts = per_seq * cache->num_seqs;
-    p.qscale = float(double(scale) * 1.4426950408889634);  // log2(e)
+    // (a positive number: a hidden row's logit of -infinity times it stays that)
+    p.qscale = float(std::clamp(std::fabs(double(scale)) * 1.4426950408889634, double(FLT_MIN), double(FLT_MAX)));  // log2(e)
+    p.flip = scale < 0 ? 0x80000000u : 0u;
     p.group = cache->num_q_heads / cache->num_kv_heads;
     p.max_rows = max_rows;
     p.splits = a.splits;

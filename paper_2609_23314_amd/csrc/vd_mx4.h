@@ -44,7 +44,8 @@ struct MxAttnParams {
     int64_t qs[4], os[4];      // strides (sequence, layer, query head, row) in bytes
     float *ws_acc;             // [unit][split][query row][D] unnormalised sums of the values
     float *ws_ml;              // [unit][split][query row][2] largest logit (log2 units), sum of the weights
-    float qscale;              // softmax scale times log2(e)
+    float qscale;              // size of the softmax scale times log2(e), > 0
+    uint32_t flip;             // sign bit of the softmax scale
     int32_t group;             // query heads per KV head
     int32_t max_rows, splits, tiles;
     int32_t block;             // the kernel for blocks of query rows, its tiles of kMxBlockTile

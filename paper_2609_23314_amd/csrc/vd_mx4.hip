@@ -204,17 +204,20 @@ __device__ __forceinline__ Scales<D> load_scales(const char *row) {
     return r;
 }
 
-// Eight channels of a query row, in parts.
+// Eight channels of a query row, in parts; `flip` turns their signs (a negative
+// softmax scale, so that a larger product is always a larger logit).
 template <int DTYPE, int QP, int FRAGS>
-__device__ __forceinline__ void load_query(bf16x8 (&q)[QP][FRAGS], int f, const char *row, int ch) {
+__device__ __forceinline__ void load_query(bf16x8 (&q)[QP][FRAGS], int f, const char *row, int ch, uint32_t flip) {
     if (DTYPE == VD_DTYPE_BF16) {
-        q[0][f] = *reinterpret_cast<const bf16x8 *>(row + ch * 2);
+        const u32x4 x = *reinterpret_cast<const u32x4 *>(row + ch * 2);
+        const uint32_t both = flip | flip >> 16;
+        q[0][f] = __builtin_bit_cast(bf16x8, x ^ both);
         return;
     }
     const f32x4 a = *reinterpret_cast<const f32x4 *>(row + ch * 4), b = *reinterpret_cast<const f32x4 *>(row + ch * 4 + 16);
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-        float x = e < 4 ? a[e & 3] : b[e & 3];
+        float x = as_float(bits(e < 4 ? a[e & 3] : b[e & 3]) ^ flip);
 #pragma unroll
         for (int part = 0; part < QP; ++part) {
             q[part][f][e] = __bf16(x);
@@ -259,7 +262,7 @@ __global__ __launch_bounds__(kMxThreads) void attn_kernel(const MxAttnParams p) 
     {
         const char *src = p.q + s * p.qs[0] + layer * p.qs[1] + (head * G + g) * p.qs[2] + i * p.qs[3];
 #pragma unroll
-        for (int f = 0; f < FRAGS; ++f) load_query<DTYPE, QP>(q, f, src, kq * (D / 4) + 8 * f);
+        for (int f = 0; f < FRAGS; ++f) load_query<DTYPE, QP>(q, f, src, kq * (D / 4) + 8 * f, p.flip);
     }
 
     const char *kb = p.c.k + s * p.c.seq + layer * p.c.layer + head * p.c.head;
@@ -305,17 +308,16 @@ __global__ __launch_bounds__(kMxThreads) void attn_kernel(const MxAttnParams p) 
             }
         }
         // lane: query c, rows j0 + 16 t + 4 kq + r
-        float best = -INFINITY;
-        const bool masked = j0 + 32 > min(all_see, end);
+        if (j0 + 32 > min(all_see, end)) {
 #pragma unroll
-        for (int t = 0; t < 2; ++t)
+            for (int t = 0; t < 2; ++t)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                float x = z[t][r] * p.qscale;
-                if (masked) x = j0 + 16 * t + 4 * kq + r < min(limit, end) ? x : -INFINITY;
-                z[t][r] = x;
-                best = fmaxf(best, x);
-            }
+                for (int r = 0; r < 4; ++r) z[t][r] = j0 + 16 * t + 4 * kq + r < min(limit, end) ? z[t][r] : -INFINITY;
+        }
+        float best = z[0][0];
+#pragma unroll
+        for (int e = 1; e < 8; ++e) best = fmaxf(best, z[e >> 2][e & 3]);
+        best *= p.qscale;
         // The weights are relative to a maximum that is raised only when a logit
         // passes it by 8 (log2 units): they stay below 2^8, and mostly no sum is rescaled.
         if (__builtin_amdgcn_ballot_w64(best > top + 8.0f)) {
@@ -333,7 +335,7 @@ __global__ __launch_bounds__(kMxThreads) void attn_kernel(const MxAttnParams p) 
         bf16x8 w[PP];
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            float x = __builtin_amdgcn_exp2f(z[e >> 2][e & 3] - sub);
+            float x = __builtin_amdgcn_exp2f(fmaf(z[e >> 2][e & 3], p.qscale, -sub));
 #pragma unroll
             for (int part = 0; part < PP; ++part) {
                 w[part][e] = __bf16(x);
@@ -413,7 +415,18 @@ __global__ __launch_bounds__(kMxThreads) void attn_kernel(const MxAttnParams p) 
 template <int D>
 constexpr int kBlockRows = D == 256 ? 32 : 64;
 template <int D>
-constexpr int kBlockBytes = 2 * kBlockRows<D> * kVStride<D>;   // K's tile, then V's
+constexpr int kKStride = D * 2 + 16;   // sixteen rows' 16-byte reads fall into different banks
+template <int D>
+constexpr int kBlockBytes = kBlockRows<D> * (kKStride<D> + D * 2);   // K's tile, then V's
+
+// V's tile has no padding: where four rows are read together 64 bytes wide, and
+// sixteen lanes write 16 bytes each, both meet every bank once if a row's 64-byte
+// units and their 16-byte pieces change places with the row.
+template <int D>
+__device__ __forceinline__ int v_place(int row, int unit, int piece) {
+    const int u = D == 64 ? (row >> 1) & 1 : row & 3, c = D == 64 ? (row >> 1) & 3 : row & 3;
+    return row * (D * 2) + ((unit ^ u) * 64) + ((piece ^ c) * 16);
+}
 
 // A thread's part of a tile on its way from memory: groups of K, then groups of V
 // (of D = 64 one group of either).
@@ -450,9 +463,10 @@ struct BlockStage {
             } else {
                 byte = ks[i % K_ITEMS].has_nan() || vs[i % K_ITEMS].has_nan() ? 255u : ks[i % K_ITEMS].byte(group);
             }
-            char *to = tile + (is_v(i) ? ROWS * kVStride<D> : 0) + row * kVStride<D> + group * 64;
 #pragma unroll
-            for (int w = 0; w < 4; ++w) reinterpret_cast<bf16x8 *>(to)[w] = decode8(x[i][w], scale_of(byte));
+            for (int w = 0; w < 4; ++w)
+                *reinterpret_cast<bf16x8 *>(tile + (is_v(i) ? ROWS * kKStride<D> + v_place<D>(row, group, w)
+                                                            : row * kKStride<D> + group * 64 + 16 * w)) = decode8(x[i][w], scale_of(byte));
         }
     }
 };
@@ -485,7 +499,7 @@ __global__ __launch_bounds__(kMxThreads, 2) void attn_block_kernel(const MxAttnP
     {
         const char *src = p.q + s * p.qs[0] + layer * p.qs[1] + (head * G + g) * p.qs[2] + i * p.qs[3];
 #pragma unroll
-        for (int f = 0; f < FRAGS; ++f) load_query<DTYPE, QP>(q, f, src, 16 * f + 8 * half);
+        for (int f = 0; f < FRAGS; ++f) load_query<DTYPE, QP>(q, f, src, 16 * f + 8 * half, p.flip);
     }
     const char *kb = p.c.k + s * p.c.seq + layer * p.c.layer + head * p.c.head;
     const char *vb = p.c.v + s * p.c.seq + layer * p.c.layer + head * p.c.head;
@@ -500,6 +514,12 @@ __global__ __launch_bounds__(kMxThreads, 2) void attn_block_kernel(const MxAttnP
     float top = -INFINITY, sub = 0.0f, sum = 0.0f;   // (the sum of the lane's rows)
     const bf16x2 ones = {__bf16(1.0f), __bf16(1.0f)};
 
+    // where the lane's turned reads of V start (the rows of a tile that differ by 8 have their places alike)
+    int v_at[CT < 4 ? CT : 4];
+#pragma unroll
+    for (int ct = 0; ct < (CT < 4 ? CT : 4); ++ct)
+        v_at[ct] = v_place<D>(4 * half + ((lane & 15) >> 2), ct, 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) + (lane & 1) * 8;
+
     BlockStage<D> stage;
     if (begin < end) {
         stage.load(kb, vb, ksb, vsb, p.c.slot, p.c.sslot, begin, end);
@@ -510,7 +530,7 @@ __global__ __launch_bounds__(kMxThreads, 2) void attn_block_kernel(const MxAttnP
     for (int j0 = begin; j0 < end; j0 += T) {
         const bool more = j0 + T < end;
         if (more) stage.load(kb, vb, ksb, vsb, p.c.slot, p.c.sslot, j0 + T, end);
-        const char *kt = lds + buffer * kBlockBytes<D>, *vt = kt + T * kVStride<D>;
+        const char *kt = lds + buffer * kBlockBytes<D>, *vt = kt + T * kKStride<D>;
         if (j0 < wave_end) {
             f32x16 z[SUBS];
 #pragma unroll
@@ -519,32 +539,24 @@ __global__ __launch_bounds__(kMxThreads, 2) void attn_block_kernel(const MxAttnP
                 for (int r = 0; r < 16; ++r) z[t][r] = 0.0f;
 #pragma unroll
                 for (int f = 0; f < FRAGS; ++f) {
-                    const bf16x8 a = *reinterpret_cast<const bf16x8 *>(kt + (32 * t + c) * kVStride<D> + (16 * f + 8 * half) * 2);
+                    const bf16x8 a = *reinterpret_cast<const bf16x8 *>(kt + (32 * t + c) * kKStride<D> + (16 * f + 8 * half) * 2);
 #pragma unroll
                     for (int part = QP - 1; part >= 0; --part)
                         z[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, q[part][f], z[t], 0, 0, 0);
                 }
             }
             // lane: query c, rows j0 + 32 t + 8 (r / 4) + 4 half + r % 4
-            float best = -INFINITY;
             if (j0 + T > all_see) {
 #pragma unroll
                 for (int t = 0; t < SUBS; ++t)
 #pragma unroll
-                    for (int r = 0; r < 16; ++r) {
-                        const int j = j0 + 32 * t + 8 * (r >> 2) + 4 * half + (r & 3);
-                        z[t][r] = j < limit ? z[t][r] * p.qscale : -INFINITY;
-                        best = fmaxf(best, z[t][r]);
-                    }
-            } else {
-#pragma unroll
-                for (int t = 0; t < SUBS; ++t)
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) {
-                        z[t][r] *= p.qscale;
-                        best = fmaxf(best, z[t][r]);
-                    }
+                    for (int r = 0; r < 16; ++r)
+                        z[t][r] = j0 + 32 * t + 8 * (r >> 2) + 4 * half + (r & 3) < limit ? z[t][r] : -INFINITY;
             }
+            float best = z[0][0];
+#pragma unroll
+            for (int e = 1; e < 16 * SUBS; ++e) best = fmaxf(best, z[e >> 4][e & 15]);
+            best *= p.qscale;
             if (__builtin_amdgcn_ballot_w64(best > top + 8.0f)) {   // (as above)
                 best = fmaxf(best, __shfl_xor(best, 32));
                 const float next = fmaxf(top, best);
@@ -565,7 +577,7 @@ __global__ __launch_bounds__(kMxThreads, 2) void attn_block_kernel(const MxAttnP
                     bf16x8 w[PP];
 #pragma unroll
                     for (int e = 0; e < 8; ++e) {
-                        float x = __builtin_amdgcn_exp2f(z[t][8 * k + e] - sub);
+                        float x = __builtin_amdgcn_exp2f(fmaf(z[t][8 * k + e], p.qscale, -sub));
 #pragma unroll
                         for (int part = 0; part < PP; ++part) {
                             w[part][e] = __bf16(x);
@@ -582,10 +594,9 @@ __global__ __launch_bounds__(kMxThreads, 2) void attn_block_kernel(const MxAttnP
 #pragma unroll
                     for (int ct = 0; ct < CT; ++ct) {
                         typedef __attribute__((address_space(3))) s16x4 *lds4;
-                        const char *at = vt + (32 * t + 16 * k + 4 * half + ((lane & 15) >> 2)) * kVStride<D> + ct * 64 +
-                                         ((lane >> 4) & 1) * 32 + (lane & 3) * 8;
+                        const char *at = vt + v_at[ct & 3] + (ct >> 2) * 256 + (32 * t + 16 * k) * (D * 2);
                         const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(at));
-                        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(at + 8 * kVStride<D>));
+                        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(at + 8 * (D * 2)));
                         const bf16x8 a = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
 #pragma unroll
                         for (int part = PP - 1; part >= 0; --part)

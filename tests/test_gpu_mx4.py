@@ -263,6 +263,16 @@ def test_attention_nan_rows_stay_with_their_queries(dtype, D, side, t, G):
     assert out[:, :, :, sees].isnan().all() and torch.equal(out[:, :, :, ~sees], clean[:, :, :, ~sees])
 
 
+@pytest.mark.parametrize("scale", [-0.3, 0.0, 1e-3])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("t", [2, 40])
+def test_attention_scales(scale, dtype, t):
+    """A negative softmax scale, and one of zero (the mean of the rows seen)."""
+    cache = _cache(1, 1, 1, 130, 128, 67)
+    q = _rows((1, 1, 2, t, 128), dtype, 68, 0.3).to(DEV)
+    _check_attention(cache, q, [130], [t], vd.vd_attention_mx4(cache, q, [130], scale=scale), scale)
+
+
 def test_attention_nonfinite_queries():
     """A query row with NaN or an infinity spoils its own output alone."""
     cache = _cache(1, 1, 1, 200, 128, 65)
