@@ -161,11 +161,10 @@ AttnPlan attn_plan(const vd_mx4_cache *c, int32_t dtype, int64_t max_rows, int64
     const int64_t queries = max_rows * (c->num_q_heads / c->num_kv_heads);
     const int64_t units = int64_t(c->num_seqs) * c->num_layers * c->num_kv_heads;
     AttnPlan a;
-    // (three parts of 256 channels of a query do not fit the block kernel's registers)
-    a.block = queries > vd::kMxTile && !(dtype == VD_DTYPE_F32 && c->head_dim == 256);
+    a.block = queries > vd::kMxTile;
     const int64_t tile = a.block ? vd::kMxBlockTile : vd::kMxTile;
     a.tiles = int((queries + tile - 1) / tile);
-    const int64_t groups = units * a.tiles, resident = (a.block ? 2 : 4) * 256;
+    const int64_t groups = units * a.tiles, resident = (a.block ? vd::block_groups(dtype, c->head_dim) : 4) * 256;
     a.splits = int(std::max<int64_t>(1, std::min<int64_t>({vd::kMxMaxSplits, resident / groups, n / 256})));
     return a;
 }

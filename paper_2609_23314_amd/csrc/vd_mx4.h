@@ -14,7 +14,10 @@ constexpr int kMxThreads = 256;   // threads of an append, read or attention wor
 constexpr int kMxEvictThreads = 1024;
 constexpr int kMxTile = 16;       // query rows of the attention kernel's tile
 constexpr int kMxBlockTile = 128; // and of the one for blocks of them
-constexpr int kMxMaxSplits = 64;  // the combining wave holds a split per lane
+// its workgroups on a CU: with one wave a SIMD the sums and queries of 256 channels, or
+// the three parts of 128, stay in registers
+constexpr int block_groups(int dtype, int head_dim) { return head_dim == 256 || (dtype == 1 && head_dim == 128) ? 1 : 2; }
+constexpr int kMxMaxSplits = 128; // two for each lane of a joining wave
 
 // A 4-bit cache as the kernels see it: bases of the launch's first sequence,
 // strides in bytes.  A unit's slab spans < 4 GiB.

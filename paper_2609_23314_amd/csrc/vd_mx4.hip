@@ -184,10 +184,11 @@ struct Scales {
         const uint32_t x = WORDS == 2 && group >= 4 ? w[WORDS - 1] : w[0];
         return (x >> (8 * (group & 3))) & 255u;
     }
-    __device__ __forceinline__ bool has_nan() const {
-        bool nan = false;
-        for (int i = 0; i < WORDS; ++i) nan |= ((~w[i] - 0x01010101u) & w[i] & 0x80808080u) != 0;   // a zero byte of ~w
-        return nan;
+    // 255 if any of the row's groups is NaN, else 0
+    __device__ __forceinline__ uint32_t nan_bits() const {
+        uint32_t nan = 0;
+        for (int i = 0; i < WORDS; ++i) nan |= (~w[i] - 0x01010101u) & w[i] & 0x80808080u;   // a zero byte of ~w
+        return nan ? 255u : 0u;
     }
 };
 template <int D>
@@ -292,12 +293,12 @@ __global__ __launch_bounds__(kMxThreads) void attn_kernel(const MxAttnParams p) 
         f32x4 z[2];
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
-            const bool nan = ks[t].has_nan() || vs[t].has_nan();
+            const uint32_t nan = ks[t].nan_bits() | vs[t].nan_bits();
             z[t] = f32x4{0, 0, 0, 0};
 #pragma unroll
             for (int f = 0; f < FRAGS; ++f) {
                 const int group = (kq * (D / 4) + 8 * f) / kMxGroup;
-                const float scale = scale_of(nan ? 255u : ks[t].byte(group));
+                const float scale = scale_of(ks[t].byte(group) | nan);
                 const bf16x8 a = decode8(kc[t].w[f], scale);
 #pragma unroll
                 for (int part = QP - 1; part >= 0; --part)
@@ -412,12 +413,11 @@ __global__ __launch_bounds__(kMxThreads) void attn_kernel(const MxAttnParams p) 
 // With v_mfma_f32_32x32x16_bf16 as above, transposed: a lane holds one query's
 // logits of 16 rows of 32, which are the right operand of the product with V^T.
 
-template <int D>
-constexpr int kBlockRows = D == 256 ? 32 : 64;
+constexpr int kBlockRows = 64;
 template <int D>
 constexpr int kKStride = D * 2 + 16;   // sixteen rows' 16-byte reads fall into different banks
 template <int D>
-constexpr int kBlockBytes = kBlockRows<D> * (kKStride<D> + D * 2);   // K's tile, then V's
+constexpr int kBlockBytes = kBlockRows * (kKStride<D> + D * 2);   // K's tile, then V's
 
 // V's tile has no padding: where four rows are read together 64 bytes wide, and
 // sixteen lanes write 16 bytes each, both meet every bank once if a row's 64-byte
@@ -432,17 +432,18 @@ __device__ __forceinline__ int v_place(int row, int unit, int piece) {
 // (of D = 64 one group of either).
 template <int D>
 struct BlockStage {
-    static constexpr int GROUPS = D / 32, ROWS = kBlockRows<D>, ITEMS = 2 * ROWS * GROUPS / kMxThreads, K_ITEMS = (ITEMS + 1) / 2;
+    static constexpr int GROUPS = D / 32, ROWS = kBlockRows, ITEMS = 2 * ROWS * GROUPS / kMxThreads, K_ITEMS = (ITEMS + 1) / 2;
     u32x4 x[ITEMS];
     Scales<D> ks[K_ITEMS], vs[K_ITEMS];   // of the whole row, whose NaN groups K's items look for
     uint32_t vbyte[ITEMS];                // of V's items
     __device__ __forceinline__ static bool is_v(int i) { return ITEMS == 1 ? int(threadIdx.x) >= ROWS * GROUPS : i >= K_ITEMS; }
     __device__ __forceinline__ static int at(int i) { return (int(threadIdx.x) + i * kMxThreads) % (ROWS * GROUPS); }
+    // K's items of the tile at jk, V's of the one at jv
     __device__ __forceinline__ void load(const char *kb, const char *vb, const char *ksb, const char *vsb, uint32_t slot,
-                                         uint32_t sslot, int j0, int end) {
+                                         uint32_t sslot, int jk, int jv, int end) {
 #pragma unroll
         for (int i = 0; i < ITEMS; ++i) {
-            const uint32_t row = uint32_t(min(j0 + at(i) / GROUPS, end - 1));   // behind the end: the last row, hidden later
+            const uint32_t row = uint32_t(min((is_v(i) ? jv : jk) + at(i) / GROUPS, end - 1));   // behind the end: the last row, hidden later
             x[i] = reinterpret_cast<const u32x4 *>((is_v(i) ? vb : kb) + row * slot)[at(i) % GROUPS];
             if (i < K_ITEMS) {
                 ks[i % K_ITEMS] = load_scales<D>(ksb + row * sslot);
@@ -452,22 +453,19 @@ struct BlockStage {
             }
         }
     }
-    __device__ __forceinline__ void store(char *tile) const {
-#pragma unroll
-        for (int i = 0; i < ITEMS; ++i) {
+    __device__ __forceinline__ void store(int i, char *kt, char *vt) const {
             const int row = at(i) / GROUPS, group = at(i) % GROUPS;
             uint32_t byte;
             if (is_v(i)) {
                 byte = i < K_ITEMS ? vs[i % K_ITEMS].byte(group) : vbyte[i];
                 byte = byte == 255u ? 0u : byte;
             } else {
-                byte = ks[i % K_ITEMS].has_nan() || vs[i % K_ITEMS].has_nan() ? 255u : ks[i % K_ITEMS].byte(group);
+                byte = ks[i % K_ITEMS].byte(group) | ks[i % K_ITEMS].nan_bits() | vs[i % K_ITEMS].nan_bits();
             }
 #pragma unroll
             for (int w = 0; w < 4; ++w)
-                *reinterpret_cast<bf16x8 *>(tile + (is_v(i) ? ROWS * kKStride<D> + v_place<D>(row, group, w)
-                                                            : row * kKStride<D> + group * 64 + 16 * w)) = decode8(x[i][w], scale_of(byte));
-        }
+                *reinterpret_cast<bf16x8 *>(is_v(i) ? vt + v_place<D>(row, group, w) : kt + row * kKStride<D> + group * 64 + 16 * w) =
+                    decode8(x[i][w], scale_of(byte));
     }
 };
 
@@ -475,8 +473,8 @@ __device__ __forceinline__ float dot2(bf16x2 a, bf16x2 b, float c) { return __bu
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 template <int DTYPE, int D>
-__global__ __launch_bounds__(kMxThreads, 2) void attn_block_kernel(const MxAttnParams p) {
-    constexpr int FRAGS = D / 16, CT = D / 32, SUBS = kBlockRows<D> / 32;
+__global__ __launch_bounds__(kMxThreads, block_groups(DTYPE, D)) void attn_block_kernel(const MxAttnParams p) {
+    constexpr int FRAGS = D / 16, CT = D / 32, SUBS = kBlockRows / 32;
     constexpr int QP = DTYPE == VD_DTYPE_F32 ? 3 : 1, PP = DTYPE == VD_DTYPE_F32 ? 2 : 1;
     __shared__ __attribute__((aligned(16))) char lds[2 * kBlockBytes<D>];
     const int split = blockIdx.x / p.tiles, tile = blockIdx.x % p.tiles;
@@ -486,14 +484,13 @@ __global__ __launch_bounds__(kMxThreads, 2) void attn_block_kernel(const MxAttnP
     if (m0 >= queries) return;
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, c = lane & 31, half = lane >> 5;
     const int seen = max(0, n - rows + 1 + min(m0 + kMxBlockTile - 1, queries - 1) / G);
-    constexpr int T = kBlockRows<D>;
+    constexpr int T = kBlockRows;
     const int share = ((seen + p.splits - 1) / p.splits + T - 1) / T * T;
     const int begin = min(split * share, seen), end = min(begin + share, seen);
     const int wm0 = m0 + 32 * wave, m = wm0 + c;
     const int i = min(m, queries - 1) / G, g = min(m, queries - 1) - i * G;
     const int limit = min(n - rows + 1 + i, end);
-    const int all_see = min(n - rows + 1 + min(wm0, queries - 1) / G, end);            // rows that every query of the wave sees
-    const int wave_end = wm0 < queries ? min(n - rows + 1 + min(wm0 + 31, queries - 1) / G, end) : begin;   // and any of them
+    const int all_see = min(n - rows + 1 + min(wm0, queries - 1) / G, end);   // rows that every query of the wave sees
 
     bf16x8 q[QP][FRAGS];   // channels 16 f + 8 half + e of query c
     {
@@ -520,92 +517,126 @@ __global__ __launch_bounds__(kMxThreads, 2) void attn_block_kernel(const MxAttnP
     for (int ct = 0; ct < (CT < 4 ? CT : 4); ++ct)
         v_at[ct] = v_place<D>(4 * half + ((lane & 15) >> 2), ct, 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) + (lane & 1) * 8;
 
+    // logits of a tile: a lane has query c, rows 32 t + 8 (r / 4) + 4 half + r % 4
+    auto logits = [&](f32x16 (&z)[SUBS], const char *kt) {
+#pragma unroll
+        for (int t = 0; t < SUBS; ++t) {
+#pragma unroll
+            for (int r = 0; r < 16; ++r) z[t][r] = 0.0f;
+#pragma unroll
+            for (int f = 0; f < FRAGS; ++f) {
+                const bf16x8 a = *reinterpret_cast<const bf16x8 *>(kt + (32 * t + c) * kKStride<D> + (16 * f + 8 * half) * 2);
+#pragma unroll
+                for (int part = QP - 1; part >= 0; --part)
+                    z[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, q[part][f], z[t], 0, 0, 0);
+            }
+        }
+    };
+    // weights of sixteen rows: the right operand of the product with V
+    auto weights = [&](bf16x8 (&w)[PP], const f32x16 &z, int k) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            float x = __builtin_amdgcn_exp2f(fmaf(z[8 * k + e], p.qscale, -sub));
+#pragma unroll
+            for (int part = 0; part < PP; ++part) {
+                w[part][e] = __bf16(x);
+                x -= float(w[part][e]);
+            }
+        }
+#pragma unroll
+        for (int part = 0; part < PP; ++part) {
+            sum = dot2(__builtin_shufflevector(w[part], w[part], 0, 1), ones, sum);
+            sum = dot2(__builtin_shufflevector(w[part], w[part], 2, 3), ones, sum);
+            sum = dot2(__builtin_shufflevector(w[part], w[part], 4, 5), ones, sum);
+            sum = dot2(__builtin_shufflevector(w[part], w[part], 6, 7), ones, sum);
+        }
+    };
+    auto read_values = [&](bf16x8 (&a)[CT], const char *vt, int step) {   // sixteen rows of V, turned
+#pragma unroll
+        for (int ct = 0; ct < CT; ++ct) {
+            typedef __attribute__((address_space(3))) s16x4 *lds4;
+            const char *at = vt + v_at[ct & 3] + (ct >> 2) * 256 + step * 16 * (D * 2);
+            const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(at));
+            const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(at + 8 * (D * 2)));
+            a[ct] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+        }
+    };
+    constexpr int KT = T * kKStride<D>, VT = T * D * 2, STEPS = SUBS * 2;
+    constexpr int ITEMS = BlockStage<D>::ITEMS;
+    char *k_lds = lds, *v_lds = lds + 2 * KT;
     BlockStage<D> stage;
     if (begin < end) {
-        stage.load(kb, vb, ksb, vsb, p.c.slot, p.c.sslot, begin, end);
-        stage.store(lds);
+        stage.load(kb, vb, ksb, vsb, p.c.slot, p.c.sslot, begin, begin, end);
+#pragma unroll
+        for (int i = 0; i < ITEMS; ++i) stage.store(i, k_lds, v_lds);
     }
     __syncthreads();
     int buffer = 0;
-    for (int j0 = begin; j0 < end; j0 += T) {
-        const bool more = j0 + T < end;
-        if (more) stage.load(kb, vb, ksb, vsb, p.c.slot, p.c.sslot, j0 + T, end);
-        const char *kt = lds + buffer * kBlockBytes<D>, *vt = kt + T * kKStride<D>;
-        if (j0 < wave_end) {
-            f32x16 z[SUBS];
+    for (int j0 = begin; j0 < end; j0 += T, buffer ^= 1) {
+        stage.load(kb, vb, ksb, vsb, p.c.slot, p.c.sslot, j0 + T, j0 + T, end);   // (behind the last tile: not used)
+        const char *vt = v_lds + buffer * VT;
+        f32x16 now[SUBS];
+        logits(now, k_lds + buffer * KT);
+        bf16x8 va[2][CT], w[2][PP];
+        read_values(va[0], vt, 0);
+        // the next tile's loads first, and the matrix cores' operands read well ahead of the products
+        __builtin_amdgcn_sched_group_barrier(0x020, 16, 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, 8, 0);
 #pragma unroll
-            for (int t = 0; t < SUBS; ++t) {
-#pragma unroll
-                for (int r = 0; r < 16; ++r) z[t][r] = 0.0f;
-#pragma unroll
-                for (int f = 0; f < FRAGS; ++f) {
-                    const bf16x8 a = *reinterpret_cast<const bf16x8 *>(kt + (32 * t + c) * kKStride<D> + (16 * f + 8 * half) * 2);
-#pragma unroll
-                    for (int part = QP - 1; part >= 0; --part)
-                        z[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, q[part][f], z[t], 0, 0, 0);
-                }
-            }
-            // lane: query c, rows j0 + 32 t + 8 (r / 4) + 4 half + r % 4
-            if (j0 + T > all_see) {
-#pragma unroll
-                for (int t = 0; t < SUBS; ++t)
-#pragma unroll
-                    for (int r = 0; r < 16; ++r)
-                        z[t][r] = j0 + 32 * t + 8 * (r >> 2) + 4 * half + (r & 3) < limit ? z[t][r] : -INFINITY;
-            }
-            float best = z[0][0];
-#pragma unroll
-            for (int e = 1; e < 16 * SUBS; ++e) best = fmaxf(best, z[e >> 4][e & 15]);
-            best *= p.qscale;
-            if (__builtin_amdgcn_ballot_w64(best > top + 8.0f)) {   // (as above)
-                best = fmaxf(best, __shfl_xor(best, 32));
-                const float next = fmaxf(top, best);
-                const float to = next == -INFINITY ? 0.0f : next;
-                const float down = __builtin_amdgcn_exp2f(top - to);
-                top = next;
-                sub = to;
-                sum *= down;
-#pragma unroll
-                for (int t = 0; t < CT; ++t)
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) acc[t][r] *= down;
-            }
+        for (int i = 0; i < SUBS * FRAGS; ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x008, QP, 0);
+            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+        }
+        if (j0 + T > all_see) {
 #pragma unroll
             for (int t = 0; t < SUBS; ++t)
 #pragma unroll
-                for (int k = 0; k < 2; ++k) {   // sixteen rows
-                    bf16x8 w[PP];
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        float x = __builtin_amdgcn_exp2f(fmaf(z[t][8 * k + e], p.qscale, -sub));
-#pragma unroll
-                        for (int part = 0; part < PP; ++part) {
-                            w[part][e] = __bf16(x);
-                            x -= float(w[part][e]);
-                        }
-                    }
-#pragma unroll
-                    for (int part = 0; part < PP; ++part) {
-                        sum = dot2(__builtin_shufflevector(w[part], w[part], 0, 1), ones, sum);
-                        sum = dot2(__builtin_shufflevector(w[part], w[part], 2, 3), ones, sum);
-                        sum = dot2(__builtin_shufflevector(w[part], w[part], 4, 5), ones, sum);
-                        sum = dot2(__builtin_shufflevector(w[part], w[part], 6, 7), ones, sum);
-                    }
-#pragma unroll
-                    for (int ct = 0; ct < CT; ++ct) {
-                        typedef __attribute__((address_space(3))) s16x4 *lds4;
-                        const char *at = vt + v_at[ct & 3] + (ct >> 2) * 256 + (32 * t + 16 * k) * (D * 2);
-                        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(at));
-                        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(at + 8 * (D * 2)));
-                        const bf16x8 a = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
-#pragma unroll
-                        for (int part = PP - 1; part >= 0; --part)
-                            acc[ct] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, w[part], acc[ct], 0, 0, 0);
-                    }
-                }
+                for (int r = 0; r < 16; ++r)
+                    now[t][r] = j0 + 32 * t + 8 * (r >> 2) + 4 * half + (r & 3) < limit ? now[t][r] : -INFINITY;
         }
-        buffer ^= 1;
-        if (more) stage.store(lds + buffer * kBlockBytes<D>);
+        float best = now[0][0];
+#pragma unroll
+        for (int e = 1; e < 16 * SUBS; ++e) best = fmaxf(best, now[e >> 4][e & 15]);
+        best *= p.qscale;
+        if (__builtin_amdgcn_ballot_w64(best > top + 8.0f)) {   // (as above)
+            best = fmaxf(best, __shfl_xor(best, 32));
+            const float next = fmaxf(top, best);
+            const float to = next == -INFINITY ? 0.0f : next;
+            const float down = __builtin_amdgcn_exp2f(top - to);
+            top = next;
+            sub = to;
+            sum *= down;
+#pragma unroll
+            for (int t = 0; t < CT; ++t)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) acc[t][r] *= down;
+        }
+        // Sixteen rows at a time: the products with V stand between the arithmetic of the
+        // next sixteen rows' weights, or, at the end, of the next tile's conversion.
+        weights(w[0], now[0], 0);
+#pragma unroll
+        for (int step = 0; step < STEPS; ++step) {
+            __builtin_amdgcn_sched_barrier(0);
+            if (step + 1 < STEPS) {
+                read_values(va[(step + 1) & 1], vt, step + 1);
+                weights(w[(step + 1) & 1], now[(step + 1) >> 1], (step + 1) & 1);
+            }
+#pragma unroll
+            for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+                for (int part = PP - 1; part >= 0; --part)
+                    acc[ct] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(va[step & 1][ct], w[step & 1][part], acc[ct], 0, 0, 0);
+#pragma unroll
+            for (int i = 0; i < ITEMS; ++i)
+                if (step == max(STEPS - ITEMS, 0) + i || (step == STEPS - 1 && i >= STEPS))
+                    stage.store(i, k_lds + (buffer ^ 1) * KT, v_lds + (buffer ^ 1) * VT);
+#pragma unroll
+            for (int ct = 0; ct < CT; ++ct) {
+                __builtin_amdgcn_sched_group_barrier(0x008, PP, 0);
+                __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+                __builtin_amdgcn_sched_group_barrier(0x002, 8, 0);
+            }
+        }
         __syncthreads();
     }
     if (m >= queries) return;
@@ -630,39 +661,59 @@ __global__ __launch_bounds__(kMxThreads, 2) void attn_block_kernel(const MxAttnP
         }
 }
 
-// Joins the splits of a query row: a wave a row, a lane D / 64 channels.
-template <int DTYPE, int D>
+// Joins the splits of a query row.  WAVES waves of a workgroup take a row, of many
+// splits all four; D / 4 lanes add up a split's sums.
+template <int DTYPE, int D, int WAVES>
 __global__ __launch_bounds__(kMxThreads) void attn_join_kernel(const MxAttnParams p) {
-    constexpr int CH = D / 64;
+    constexpr int LANES = D / 4, AT_ONCE = WAVES * 64 / LANES;   // splits at a time
+    __shared__ __attribute__((aligned(16))) f32x4 sums[kMxThreads];
     const int G = p.group, lane = threadIdx.x & 63;
     const int head = blockIdx.y, s = blockIdx.z / p.c.layers, layer = blockIdx.z % p.c.layers;
-    const int query = blockIdx.x * (kMxThreads / 64) + (threadIdx.x >> 6);
-    if (query >= p.rows[s] * G) return;
+    const int row = threadIdx.x / (WAVES * 64), at = threadIdx.x % (WAVES * 64);
+    const int query = min(int(blockIdx.x) * (4 / WAVES) + row, p.rows[s] * G - 1);   // (behind the last: the last again, not written)
+    if (query < 0) return;                                                         // (a sequence without query rows)
     const int64_t unit = (int64_t(s) * p.c.layers + layer) * p.c.heads + head;
     const int64_t all = int64_t(p.max_rows) * G, first = unit * p.splits * all + query;
-    const bool mine = lane < p.splits;
-    const float top = mine ? p.ws_ml[(first + lane * all) * 2] : -INFINITY;
-    const float sum = mine ? p.ws_ml[(first + lane * all) * 2 + 1] : 0.0f;
-    float high = top;
-    for (int d = 1; d < 64; d *= 2) high = fmaxf(high, __shfl_xor(high, d));
-    const float f = top == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(top - high);
-    float total = sum * f;
-    for (int d = 1; d < 64; d *= 2) total += __shfl_xor(total, d);
-    float o[CH] = {};
-    for (int split = 0; split < p.splits; ++split) {
-        const float w = __shfl(f, split);
-        const float *x = p.ws_acc + (first + split * all) * D + lane * CH;
-        for (int e = 0; e < CH; ++e) o[e] = fmaf(x[e], w, o[e]);
+    float top[2], sum[2], high = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const bool mine = lane + 64 * i < p.splits;
+        const float *ml = p.ws_ml + (first + (mine ? lane + 64 * i : 0) * all) * 2;
+        top[i] = mine ? ml[0] : -INFINITY;
+        sum[i] = mine ? ml[1] : 0.0f;
+        high = fmaxf(high, top[i]);
     }
+    for (int d = 1; d < 64; d *= 2) high = fmaxf(high, __shfl_xor(high, d));
+    float total = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        top[i] = top[i] == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(top[i] - high);   // the split's factor
+        total = fmaf(sum[i], top[i], total);
+    }
+    for (int d = 1; d < 64; d *= 2) total += __shfl_xor(total, d);
+    f32x4 o = {0, 0, 0, 0};
+    const int mine = at / LANES, ch = at % LANES * 4;
+    for (int base = 0; base < p.splits; base += AT_ONCE) {
+        const int split = min(base + mine, p.splits - 1);
+        const float f0 = __shfl(top[0], split & 63), f1 = __shfl(top[1], split & 63), f = split < 64 ? f0 : f1;
+        const f32x4 x = *reinterpret_cast<const f32x4 *>(p.ws_acc + (first + split * all) * D + ch);
+        if (base + mine < p.splits)
+            for (int e = 0; e < 4; ++e) o[e] = fmaf(x[e], f, o[e]);
+    }
+    if (AT_ONCE > 1) {
+        sums[threadIdx.x] = o;
+        __syncthreads();
+        if (mine > 0) return;
+        for (int i = 1; i < AT_ONCE; ++i) o += sums[threadIdx.x + i * LANES];
+    }
+    if (int(blockIdx.x) * (4 / WAVES) + row != query) return;
     const float inv = total == 0.0f ? 0.0f : 1.0f / total;
     const int qi = query / G, qg = query - qi * G;
     char *dst = p.out + s * p.os[0] + layer * p.os[1] + (head * G + qg) * p.os[2] + qi * p.os[3];
-    for (int e = 0; e < CH; ++e) {
-        if (DTYPE == VD_DTYPE_F32)
-            reinterpret_cast<float *>(dst)[lane * CH + e] = o[e] * inv;
-        else
-            reinterpret_cast<__bf16 *>(dst)[lane * CH + e] = __bf16(o[e] * inv);
-    }
+    if (DTYPE == VD_DTYPE_F32)
+        *reinterpret_cast<f32x4 *>(dst + ch * 4) = o * inv;
+    else
+        *reinterpret_cast<bf16x4 *>(dst + ch * 2) = bf16x4{__bf16(o[0] * inv), __bf16(o[1] * inv), __bf16(o[2] * inv), __bf16(o[3] * inv)};
 }
 
 // ---------------------------------------------------------------- eviction
@@ -1069,12 +1120,12 @@ hipError_t launch_rows(const P &p, int seqs, int head_dim, F kernel, hipStream_t
 template <int DTYPE, int D>
 hipError_t launch_attn(const MxAttnParams &p, int seqs, hipStream_t stream) {
     const dim3 grid(uint32_t(p.splits) * p.tiles, p.c.heads, seqs * p.c.layers);
-    constexpr bool BLOCK = !(DTYPE == VD_DTYPE_F32 && D == 256);   // (whose registers do not hold it)
-    const hipError_t e = launch_with(p.block ? attn_block_kernel<DTYPE, BLOCK ? D : 128> : attn_kernel<DTYPE, D>, grid, kMxThreads, 0, stream, p);
+    const hipError_t e = launch_with(p.block ? attn_block_kernel<DTYPE, D> : attn_kernel<DTYPE, D>, grid, kMxThreads, 0, stream, p);
     if (e != hipSuccess || p.splits == 1) return e;
-    const uint32_t per = kMxThreads / 64;
-    const dim3 join((uint32_t(p.max_rows) * p.group + per - 1) / per, p.c.heads, seqs * p.c.layers);
-    return launch_with(attn_join_kernel<DTYPE, D>, join, kMxThreads, 0, stream, p);
+    const bool many = p.splits > 8;
+    const uint32_t per = many ? 1 : 4, queries = uint32_t(p.max_rows) * p.group;
+    return launch_with(many ? attn_join_kernel<DTYPE, D, 4> : attn_join_kernel<DTYPE, D, 1>,
+                       dim3((queries + per - 1) / per, p.c.heads, seqs * p.c.layers), kMxThreads, 0, stream, p);
 }
 
 template <int D>
