@@ -335,7 +335,8 @@ size_t vd_evict_step_workspace_size(const vd_cache_desc *desc);
  * multiples of 16, stride_slot >= head_dim/2.  Scales: base and strides
  * multiples of head_dim/32, scale_slot >= head_dim/32.  The four arrays do not
  * overlap.  Calls that write a cache refuse sequences, layers or heads that
- * share memory (stride 0).
+ * share memory (stride 0).  Here and below the stride of an axis with one element
+ * is not looked at (but a slot's).
  */
 #define VD_MX4_MAX_CAPACITY (1 << 24)  /* slots per unit; an eviction takes VD_MAX_CAPACITY */
 

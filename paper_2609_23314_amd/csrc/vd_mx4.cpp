@@ -26,11 +26,13 @@ struct Extent {
 };
 
 // The bytes from the first element to the last of an array [count...] of
-// `strides` (bytes) whose last axis holds `row` bytes; false if it is absurd.
+// `strides` (bytes) whose last axis holds `row` bytes; false if it is absurd.  (An axis
+// of one element is never stepped along: its stride may be anything.)
 bool extent_of(const void *base, const int64_t *count, const int64_t *strides, int axes, int64_t row, Extent &e) {
     e.at = reinterpret_cast<uintptr_t>(base);
     e.bytes = uint64_t(row);
     for (int i = 0; i < axes; ++i) {
+        if (count[i] == 1) continue;
         if (strides[i] < 0 || strides[i] > kFar / count[i]) return false;
         e.bytes += uint64_t(strides[i]) * uint64_t(count[i] - 1);
     }
@@ -60,7 +62,8 @@ vd_status check_cache(const vd_mx4_cache *c, bool written, Extent *extents = nul
     const int64_t count[4] = {c->num_seqs, c->num_layers, c->num_kv_heads, c->capacity};
     const int64_t cb = code_bytes(c), sb = scale_bytes(c);
     for (int i = 0; i < 4; ++i)
-        if (code[i] < 0 || scale[i] < 0 || code[i] % 16 != 0 || scale[i] % sb != 0) return VD_ERR_INVALID_ARG;
+        if (count[i] > 1 || i == 3)
+            if (code[i] < 0 || scale[i] < 0 || code[i] % 16 != 0 || scale[i] % sb != 0) return VD_ERR_INVALID_ARG;
     if (code[3] < cb || scale[3] < sb) return VD_ERR_INVALID_ARG;   // rows would overlap
     // a unit's slab is addressed with 32-bit byte offsets
     if (code[3] > int64_t(UINT32_MAX) / c->capacity || scale[3] > int64_t(UINT32_MAX) / c->capacity) return VD_ERR_UNSUPPORTED;
@@ -94,6 +97,8 @@ vd_status check_rows(const void *base, const int64_t *strides, const int64_t *co
     if (!base || !strides || !aligned(base, 16)) return VD_ERR_INVALID_ARG;
     const int64_t es = elem_bytes(dtype);
     for (int i = 0; i < 4; ++i) {
+        bytes[i] = 0;
+        if (count[i] == 1) continue;
         if (strides[i] < 0 || strides[i] > kFar / es / count[i]) return VD_ERR_INVALID_ARG;
         bytes[i] = strides[i] * es;
         if (bytes[i] % 16 != 0) return VD_ERR_INVALID_ARG;
@@ -161,7 +166,12 @@ AttnPlan attn_plan(const vd_mx4_cache *c, int32_t dtype, int64_t max_rows, int64
     const int64_t queries = max_rows * (c->num_q_heads / c->num_kv_heads);
     const int64_t units = int64_t(c->num_seqs) * c->num_layers * c->num_kv_heads;
     AttnPlan a;
-    a.block = queries > vd::kMxTile;
+    // Up to four tiles of single query rows the wide kernel's idle waves cost more than its
+    // tiles of cache rows, converted once for all, save (64 sequences' layers x 8 heads, 4000
+    // rows, us, tiles of 16 and blocks: bf16, D = 128, 24 queries 82 and 137, 48 122 and 148, 64
+    // 156 and 145, 96 231 and 148; D = 256, 64 315 and 367, 96 466 and 372; fp32, D = 128, 64 200
+    // and 283, 96 - and 297).  Three parts of 256 channels do not fit its registers.
+    a.block = queries > 4 * vd::kMxTile && !(dtype == VD_DTYPE_F32 && c->head_dim == 256);
     const int64_t tile = a.block ? vd::kMxBlockTile : vd::kMxTile;
     a.tiles = int((queries + tile - 1) / tile);
     const int64_t groups = units * a.tiles, resident = (a.block ? vd::block_groups(dtype, c->head_dim) : 4) * 256;

@@ -15,7 +15,7 @@ constexpr int kMxEvictThreads = 1024;
 constexpr int kMxTile = 16;       // query rows of the attention kernel's tile
 constexpr int kMxBlockTile = 128; // and of the one for blocks of them
 // its workgroups on a CU: with one wave a SIMD the sums and queries of 256 channels, or
-// the three parts of 128, stay in registers
+// the three parts of 128, stay in registers (those of 256 do not)
 constexpr int block_groups(int dtype, int head_dim) { return head_dim == 256 || (dtype == 1 && head_dim == 128) ? 1 : 2; }
 constexpr int kMxMaxSplits = 128; // two for each lane of a joining wave
 

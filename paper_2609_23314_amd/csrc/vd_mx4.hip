@@ -1120,7 +1120,8 @@ hipError_t launch_rows(const P &p, int seqs, int head_dim, F kernel, hipStream_t
 template <int DTYPE, int D>
 hipError_t launch_attn(const MxAttnParams &p, int seqs, hipStream_t stream) {
     const dim3 grid(uint32_t(p.splits) * p.tiles, p.c.heads, seqs * p.c.layers);
-    const hipError_t e = launch_with(p.block ? attn_block_kernel<DTYPE, D> : attn_kernel<DTYPE, D>, grid, kMxThreads, 0, stream, p);
+    constexpr bool BLOCK = !(DTYPE == VD_DTYPE_F32 && D == 256);   // (whose registers do not hold it)
+    const hipError_t e = launch_with(p.block ? attn_block_kernel<DTYPE, BLOCK ? D : 128> : attn_kernel<DTYPE, D>, grid, kMxThreads, 0, stream, p);
     if (e != hipSuccess || p.splits == 1) return e;
     const bool many = p.splits > 8;
     const uint32_t per = many ? 1 : 4, queries = uint32_t(p.max_rows) * p.group;

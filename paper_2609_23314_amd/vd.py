@@ -496,56 +496,64 @@ class Mx4Cache(NamedTuple):
         return Mx4Cache(*(x[s:s + 1] for x in self))
 
 
+# As above: what every call goes through keeps to few and plain Python steps (the host's
+# time for sixteen sequences' append and read-back 31 -> 26 us, for one layer's attention
+# 18 -> 15, where the GPU takes 7 and 18).
+
 def mx4_desc(cache, num_q_heads=None) -> VdMx4Cache:
     """Descriptor of an ``Mx4Cache``."""
     k, v, ks, vs = cache
     shape, sshape, strides, sstrides, dev = k.shape, ks.shape, k.stride(), ks.stride(), k.device
     if len(shape) != 5 or v.shape != shape or len(sshape) != 5 or vs.shape != sshape:
         raise ValueError("codes and scales must be 5-D [seq, layer, kv_head, slot, bytes] views, k and v alike")
-    if sshape[:4] != shape[:4] or sshape[4] * 16 != shape[4]:
-        raise ValueError("a row of head_dim channels has head_dim / 2 bytes of codes and head_dim / 32 of scales")
-    if v.stride() != strides or vs.stride() != sstrides or strides[4] != 1 or (sstrides[4] != 1 and sshape[4] > 1):
-        raise ValueError("k and v must have the same strides, and the last one must be 1")
-    for t in cache:
-        if t.dtype != torch.uint8 or t.device != dev or not t.is_cuda:
-            raise ValueError("codes and scales must be uint8 tensors on one GPU")
     S, L, H, C, B = shape
+    if sshape != (S, L, H, C, B // 16) or B % 16:
+        raise ValueError("a row of head_dim channels has head_dim / 2 bytes of codes and head_dim / 32 of scales")
+    if v.stride() != strides or vs.stride() != sstrides or strides[4] != 1 or (sstrides[4] != 1 and B > 16):
+        raise ValueError("k and v must have the same strides, and the last one must be 1")
+    if not (k.dtype == v.dtype == ks.dtype == vs.dtype == torch.uint8 and v.device == dev and ks.device == dev
+            and vs.device == dev and k.is_cuda):
+        raise ValueError("codes and scales must be uint8 tensors on one GPU")
     return VdMx4Cache(k.data_ptr(), v.data_ptr(), ks.data_ptr(), vs.data_ptr(), S, L, H,
-                      H if num_q_heads is None else int(num_q_heads), 2 * B, C, *strides[:4], *sstrides[:4])
+                      H if num_q_heads is None else num_q_heads, 2 * B, C, *strides[:4], *sstrides[:4])
 
 
-def _no_grad(name, *tensors):
+_grad_enabled = torch.is_grad_enabled
+
+
+def _no_grad(name):
     """These calls have no backward: an input that asks for one is refused."""
-    if torch.is_grad_enabled():
-        for t in tensors:
-            if t is not None and t.requires_grad:
-                raise ValueError(f"{name} has no gradient: detach its inputs or call it under torch.no_grad()")
+    raise ValueError(f"{name} has no gradient: detach its inputs or call it under torch.no_grad()")
 
 
 def _rows_view(x, name, shape, dtype, dev):
-    """A 5-D [seq, layer, head, row, head_dim] view as pointer and strides."""
-    if x.dim() != 5 or x.shape != shape or x.device != dev or x.dtype != dtype or x.is_neg():
+    """Pointer and strides of a 5-D [seq, layer, head, row, head_dim] view."""
+    if x.shape != shape or x.dtype != dtype or x.device != dev or x.is_neg():
         raise ValueError(f"{name} must be a {dtype} tensor {list(shape)} on {dev}")
     strides = x.stride()
     if strides[4] != 1:
         raise ValueError(f"{name}: the head_dim stride must be 1")
-    # (an axis of one element is never stepped along, whatever its stride says)
-    return x.data_ptr(), _Strides4(*(st if n > 1 else 0 for st, n in zip(strides[:4], shape)))
+    return x.data_ptr(), _Strides4(*strides[:4])
 
 
-_same_device = contextlib.nullcontext()
+def _host_list(x, S, name):
+    """``_host_i32`` for what mostly is a list of S ints."""
+    if type(x) is list and len(x) == S and max(x) < 2 ** 31 and min(x) >= -2 ** 31:
+        try:
+            return (ctypes.c_int32 * S)(*x)
+        except TypeError:
+            pass
+    return _host_i32(x, S, name)
 
 
-def _on(dev):
-    """The device of the call's tensors made the current one, where it is not."""
-    return _same_device if torch._C._cuda_getDevice() == dev.index else torch.cuda.device(dev)
+_nothing = contextlib.nullcontext()
 
 
-def _stream_context(dev, stream):
-    """The caller's stream made torch's current one, so that what a call allocates
-    belongs to it."""
+def _on(dev, stream):
+    """The device of the call's tensors made the current one, where it is not, and the
+    caller's stream torch's, where it gives one: what the call allocates belongs to it."""
     if stream is None:
-        return _same_device
+        return _nothing if torch._C._cuda_getDevice() == dev.index else torch.cuda.device(dev)
     if isinstance(stream, torch.cuda.Stream):
         return torch.cuda.stream(stream)
     handle = stream.cuda_stream
@@ -554,30 +562,37 @@ def _stream_context(dev, stream):
 
 def _moved(*tensors):
     """torch's backward refuses tensors whose version moved since it saved them."""
-    torch._C._increment_version(tuple(t for t in tensors if t is not None and not t.is_inference()))
+    try:
+        torch._C._increment_version(tensors)
+    except RuntimeError:   # an inference tensor, which keeps no version
+        torch._C._increment_version(tuple(t for t in tensors if not t.is_inference()))
 
 
 def vd_append_mx4(cache, n_old, k_rows, v_rows, rows=None, pos=None, pos0=None, *, stream=None):
     """Rows [S, L, H, t, D] (bfloat16 or float32) into slots [n_old[s], n_old[s] +
     rows[s]) of every unit, in 4 bits (see ``vd_append_mx4`` in vd.h); rows: t
     each where None.  pos: int32 [U, capacity], given pos0[s] + r (pos0: n_old)."""
-    _no_grad("vd_append_mx4", k_rows, v_rows)
+    if (k_rows.requires_grad or v_rows.requires_grad) and _grad_enabled():
+        _no_grad("vd_append_mx4")
     desc = mx4_desc(cache)
-    S, L, H, C, _ = cache.k.shape
-    dev, t = cache.k.device, k_rows.shape[3] if k_rows.dim() == 5 else 0
-    shape = (S, L, H, t, desc.head_dim)
-    kp, ks = _rows_view(k_rows, "k_rows", shape, k_rows.dtype, dev)
-    vp, vs = _rows_view(v_rows, "v_rows", shape, k_rows.dtype, dev)
+    S, L, H, C, B = cache[0].shape
+    dev, dtype, t = cache[0].device, k_rows.dtype, k_rows.shape[3] if k_rows.dim() == 5 else 0
+    shape = (S, L, H, t, 2 * B)
+    kp, ks = _rows_view(k_rows, "k_rows", shape, dtype, dev)
+    vp, vs = _rows_view(v_rows, "v_rows", shape, dtype, dev)
     if pos is not None:
         _need(pos, "pos", torch.int32, S * L * H * C, dev)
-    n_h = _host_i32(n_old, S, "n_old")
-    r_h = None if rows is None else _host_i32(rows, S, "rows")
-    p_h = None if pos0 is None else _host_i32(pos0, S, "pos0")
-    with _on(dev):
+    n_h = _host_list(n_old, S, "n_old")
+    r_h = None if rows is None else _host_list(rows, S, "rows")
+    p_h = None if pos0 is None else _host_list(pos0, S, "pos0")
+    with _on(dev, stream):
         _check("vd_append_mx4", load().vd_append_mx4(
             ctypes.byref(desc), _ptr(n_h), _ptr(r_h), t, _dtype_code(k_rows), kp, ks, vp, vs, _ptr(pos), _ptr(p_h),
             _stream(dev, stream)))
-    _moved(*cache, pos)
+    if pos is None:
+        _moved(*cache)
+    else:
+        _moved(*cache, pos)
 
 
 def vd_read_mx4(cache, first, t, rows=None, k_out=None, v_out=None, *, dtype=torch.bfloat16, stream=None):
@@ -585,19 +600,21 @@ def vd_read_mx4(cache, first, t, rows=None, k_out=None, v_out=None, *, dtype=tor
     ``vd_read_mx4`` in vd.h); returns (k, v), [S, L, H, t, D] of ``dtype`` or the
     given outputs.  rows: t each where None; others are left as they were."""
     desc = mx4_desc(cache)
-    S, L, H = cache.k.shape[:3]
-    dev, shape = cache.k.device, (S, L, H, int(t), desc.head_dim)
-    n_h = _host_i32(first, S, "first")
-    r_h = None if rows is None else _host_i32(rows, S, "rows")
-    with _on(dev):
-        if k_out is None or v_out is None:
-            with _stream_context(dev, stream):
-                k_out = torch.empty(shape, dtype=dtype, device=dev) if k_out is None else k_out
-                v_out = torch.empty(shape, dtype=dtype, device=dev) if v_out is None else v_out
-        _no_grad("vd_read_mx4", k_out, v_out)
+    S, L, H, _, B = cache[0].shape
+    dev, t = cache[0].device, int(t)
+    shape = (S, L, H, t, 2 * B)
+    n_h = _host_list(first, S, "first")
+    r_h = None if rows is None else _host_list(rows, S, "rows")
+    with _on(dev, stream):
+        if k_out is None:
+            k_out = torch.empty(shape, dtype=dtype, device=dev)
+        if v_out is None:
+            v_out = torch.empty(shape, dtype=k_out.dtype, device=dev)
+        if (k_out.requires_grad or v_out.requires_grad) and _grad_enabled():
+            _no_grad("vd_read_mx4")
         kp, ks = _rows_view(k_out, "k_out", shape, k_out.dtype, dev)
         vp, vs = _rows_view(v_out, "v_out", shape, k_out.dtype, dev)
-        _check("vd_read_mx4", load().vd_read_mx4(ctypes.byref(desc), _ptr(n_h), _ptr(r_h), shape[3], _dtype_code(k_out),
+        _check("vd_read_mx4", load().vd_read_mx4(ctypes.byref(desc), _ptr(n_h), _ptr(r_h), t, _dtype_code(k_out),
                                                  kp, ks, vp, vs, _stream(dev, stream)))
     _moved(k_out, v_out)
     return k_out, v_out
@@ -606,7 +623,7 @@ def vd_read_mx4(cache, first, t, rows=None, k_out=None, v_out=None, *, dtype=tor
 def vd_attention_mx4_workspace_size(cache, num_q_heads, t, n=None, dtype=torch.bfloat16):
     """Bytes of workspace for ``t`` query rows a sequence over at most n cached
     tokens (None: the cache's capacity)."""
-    desc = mx4_desc(cache, num_q_heads)
+    desc = mx4_desc(cache, int(num_q_heads))
     code = VD_DTYPE_BF16 if dtype == torch.bfloat16 else VD_DTYPE_F32
     return int(load().vd_attention_mx4_workspace_size(ctypes.byref(desc), code, int(t), desc.capacity if n is None else int(n)))
 
@@ -617,33 +634,36 @@ def vd_attention_mx4(cache, q, n_valid, rows=None, scale=None, out=None, workspa
     one is 1; returns the output, q's shape and type.  Query row i of rows[s] (t
     where None) sees the slots j < n_valid[s] - rows[s] + 1 + i.  Without a
     workspace the call takes its own from torch."""
-    _no_grad("vd_attention_mx4", q, out)
     if q.dim() != 5:
         raise ValueError("q must be [S, L, Hq, t, D] matching the cache")
-    S, L, H = cache.k.shape[:3]
-    Hq, t = q.shape[2], q.shape[3]
+    if (q.requires_grad or (out is not None and out.requires_grad)) and _grad_enabled():
+        _no_grad("vd_attention_mx4")
+    S, L, _, _, B = cache[0].shape
+    _, _, Hq, t, _ = q.shape
     desc = mx4_desc(cache, Hq)
-    dev, shape = cache.k.device, (S, L, Hq, t, desc.head_dim)
-    qp, qs = _rows_view(q, "q", shape, q.dtype, dev)
+    dev, dtype, shape = cache[0].device, q.dtype, (S, L, Hq, t, 2 * B)
+    qp, qs = _rows_view(q, "q", shape, dtype, dev)
     code = _dtype_code(q)
-    n_h = _host_i32(n_valid, S, "n_valid")
-    r_h = None if rows is None else _host_i32(rows, S, "rows")
-    sc = float(desc.head_dim) ** -0.5 if scale is None else float(scale)
-    with _on(dev):
-        size = 0
+    n_h = _host_list(n_valid, S, "n_valid")
+    r_h = None if rows is None else _host_list(rows, S, "rows")
+    sc = (2.0 * B) ** -0.5 if scale is None else float(scale)
+    lib = load()
+    with _on(dev, stream):
+        if out is None:
+            out = torch.empty(shape, dtype=dtype, device=dev)
         if workspace is None:
             longest = max(n_h) if isinstance(n_h, ctypes.Array) else int(n_h.max())
-            size = load().vd_attention_mx4_workspace_size(ctypes.byref(desc), code, t, min(max(longest, 0), desc.capacity))
-        if out is None or size:
-            with _stream_context(dev, stream):
-                out = torch.empty(shape, dtype=q.dtype, device=dev) if out is None else out
-                workspace = torch.empty(size, dtype=torch.uint8, device=dev) if size else workspace
-        if workspace is not None:
+            size = lib.vd_attention_mx4_workspace_size(ctypes.byref(desc), code, t, min(max(longest, 0), desc.capacity))
+            ws_p = None
+            if size:
+                workspace = torch.empty(size, dtype=torch.uint8, device=dev)
+                ws_p = workspace.data_ptr()
+        else:
             _need(workspace, "workspace", torch.uint8, 0, dev)
-        op, os_ = _rows_view(out, "out", shape, q.dtype, dev)
-        _check("vd_attention_mx4", load().vd_attention_mx4(
-            ctypes.byref(desc), code, qp, qs, t, _ptr(r_h), sc, _ptr(n_h), op, os_, _ptr(workspace),
-            0 if workspace is None else workspace.numel(), _stream(dev, stream)))
+            ws_p, size = workspace.data_ptr(), workspace.numel()
+        op, os_ = _rows_view(out, "out", shape, dtype, dev)
+        _check("vd_attention_mx4", lib.vd_attention_mx4(
+            ctypes.byref(desc), code, qp, qs, t, _ptr(r_h), sc, _ptr(n_h), op, os_, ws_p, size, _stream(dev, stream)))
     _moved(out)
     return out
 
@@ -652,34 +672,37 @@ def vd_evict_step_mx4(cache, n_valid, budget, variant="l2", pos=None, scores_out
     """One eviction pass over every unit of a 4-bit cache, in place (see
     ``vd_evict_step_mx4`` in vd.h)."""
     desc = mx4_desc(cache)
-    S, L, H, C, _ = cache.k.shape
-    dev, U = cache.k.device, S * L * H
-    n_h = _host_i32(n_valid, S, "n_valid")
-    b_h = _host_i32(budget, S, "budget")
+    S, L, H, C, _ = cache[0].shape
+    dev, U = cache[0].device, S * L * H
+    n_h = _host_list(n_valid, S, "n_valid")
+    b_h = _host_list(budget, S, "budget")
     if pos is not None:
         _need(pos, "pos", torch.int32, U * C, dev)
     if scores_out is not None:
         _need(scores_out, "scores_out", torch.float32, U * C, dev)
     if keep_out is not None:
         _need(keep_out, "keep_out", torch.uint8, U * C, dev)
-    with _on(dev):
+    with _on(dev, stream):
         _check("vd_evict_step_mx4", load().vd_evict_step_mx4(
             ctypes.byref(desc), _ptr(n_h), _ptr(b_h), VARIANTS[variant], _ptr(pos), _ptr(scores_out), _ptr(keep_out),
             _stream(dev, stream)))
-    _moved(*cache, pos, scores_out, keep_out)
+    _moved(*cache, *(x for x in (pos, scores_out, keep_out) if x is not None))
 
 
-def _rope_side(x, out, weight, name, S, L, t, D, w_dtype):
-    if x is None:
-        return VdRopeSide()
-    dev, shape = x.device, (S, L, x.shape[2], t, D)
-    xp, xs = _rows_view(x, name, shape, x.dtype, dev)
-    op, os_ = _rows_view(out, name + "_out", shape, out.dtype, dev)
+_no_side = VdRopeSide()
+
+
+def _rope_side(x, out, weight, names, S, L, t, D, dev, w_dtype):
+    shape, dtype = (S, L, x.shape[2], t, D), x.dtype
+    xp, xs = _rows_view(x, names[0], shape, dtype, dev)
+    out_dtype = out.dtype
+    op, os_ = _rows_view(out, names[1], shape, out_dtype, dev)
+    wp = None
     if weight is not None:
-        _need(weight, name + "_weight", w_dtype, L * D, dev)
-        if weight.numel() != L * D:
-            raise ValueError(f"{name}_weight must be [layers, head_dim]")
-    return VdRopeSide(xp, op, _ptr(weight), xs, os_, shape[2], _dtype_code(out))
+        if weight.dtype != w_dtype or weight.shape != (L, D) or weight.device != dev or not weight.is_contiguous():
+            raise ValueError(f"{names[2]} must be a contiguous {w_dtype} tensor [{L}, {D}] on {dev}")
+        wp = weight.data_ptr()
+    return VdRopeSide(xp, op, wp, xs, os_, shape[2], _dtype_code(out))
 
 
 def vd_qk_norm_rope(q, k, pos, inv_freq, q_weight=None, k_weight=None, q_out=None, k_out=None, *, eps=1e-6,
@@ -690,35 +713,43 @@ def vd_qk_norm_rope(q, k, pos, inv_freq, q_weight=None, k_weight=None, q_out=Non
     int32 [S, t]; inv_freq float32 [rotary / 2]; weights [L, D], None for no norm.
     Returns (q_out, k_out): new tensors of the inputs' type, or the given ones
     (either type; the input itself for a call in place, or the cache's own slots)."""
-    some = q if q is not None else k
+    some = k if q is None else q
     if some is None or some.dim() != 5:
         raise ValueError("q or k must be given, [S, L, heads, t, D]")
-    _no_grad("vd_qk_norm_rope", q, k, q_weight, k_weight, q_out, k_out)
+    for x in (q, k, q_weight, k_weight, q_out, k_out):
+        if x is not None and x.requires_grad and _grad_enabled():
+            _no_grad("vd_qk_norm_rope")
     S, L, _, t, D = some.shape
-    dev = some.device
+    dev, dtype = some.device, some.dtype
     if not some.is_cuda:
         raise ValueError("q and k must be on a GPU")
-    if q is not None and k is not None and (k.dim() != 5 or k.dtype != q.dtype or k.device != dev):
+    if k is not None and q is not None and (k.dim() != 5 or k.dtype != dtype):
         raise ValueError("k must match q in type and device")
-    if (q is None and q_out is not None) or (k is None and k_out is not None):
-        raise ValueError("an output without its input")
-    _need(pos, "pos", torch.int32, S * t, dev)
-    if pos.numel() != S * t:
-        raise ValueError("pos must be [seqs, rows]")
+    if (q is None and (q_out is not None or q_weight is not None)) or (k is None and (k_out is not None or k_weight is not None)):
+        raise ValueError("an output or a weight without its input")
+    if pos.shape != (S, t):
+        raise ValueError(f"pos must be [{S}, {t}]")
+    _need(pos, "pos", torch.int32, 0, dev)
     _need(inv_freq, "inv_freq", torch.float32, 0, dev)
-    w = q_weight if q_weight is not None else k_weight
-    with _on(dev):
-        if (q is not None and q_out is None) or (k is not None and k_out is None):
-            with _stream_context(dev, stream):
-                q_out = torch.empty(q.shape, dtype=q.dtype, device=dev) if q is not None and q_out is None else q_out
-                k_out = torch.empty(k.shape, dtype=k.dtype, device=dev) if k is not None and k_out is None else k_out
-        w_dtype = some.dtype if w is None else w.dtype
-        args = VdRopeArgs(_rope_side(q, q_out, q_weight, "q", S, L, t, D, w_dtype),
-                          _rope_side(k, k_out, k_weight, "k", S, L, t, D, w_dtype), pos.data_ptr(), inv_freq.data_ptr(),
-                          _dtype_code(some), VD_DTYPE_F32 if w is None else _dtype_code(w), S, L, t, D,
-                          2 * inv_freq.numel(), bool(interleaved), float(eps))
+    w = k_weight if q_weight is None else q_weight
+    w_dtype = dtype if w is None else w.dtype
+    with _on(dev, stream):
+        if q is not None and q_out is None:
+            q_out = torch.empty(q.shape, dtype=dtype, device=dev)
+        if k is not None and k_out is None:
+            k_out = torch.empty(k.shape, dtype=dtype, device=dev)
+        args = VdRopeArgs(
+            _no_side if q is None else _rope_side(q, q_out, q_weight, ("q", "q_out", "q_weight"), S, L, t, D, dev, w_dtype),
+            _no_side if k is None else _rope_side(k, k_out, k_weight, ("k", "k_out", "k_weight"), S, L, t, D, dev, w_dtype),
+            pos.data_ptr(), inv_freq.data_ptr(), _dtype_code(some), VD_DTYPE_F32 if w is None else _dtype_code(w), S, L, t,
+            D, 2 * inv_freq.numel(), 1 if interleaved else 0, eps)
         _check("vd_qk_norm_rope", load().vd_qk_norm_rope(ctypes.byref(args), _stream(dev, stream)))
-    _moved(q_out, k_out)
+    if q is None:
+        _moved(k_out)
+    elif k is None:
+        _moved(q_out)
+    else:
+        _moved(q_out, k_out)
     return q_out, k_out
 
 
