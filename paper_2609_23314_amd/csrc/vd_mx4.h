@@ -62,6 +62,7 @@ struct MxEvictParams {
     float *scores;             // the same, or null
     uint8_t *keep;             // the same, or null
     int32_t capacity, variant;
+    int32_t threads;           // of a workgroup: kMxEvictThreads or half of them
     int32_t off_lists;         // dynamic LDS: keys, then the lists from this byte on
     int32_t list_cap;          // entries of each list
     int32_t n[kMxSeqs], budget[kMxSeqs];

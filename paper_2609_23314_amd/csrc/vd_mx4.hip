@@ -6,6 +6,8 @@
 // in bf16, so that the matrix cores take a row's values without a rounding.
 #include <hip/hip_runtime.h>
 
+#include <type_traits>
+
 #include "vd.h"
 #include "vd_mx4.h"
 
@@ -728,14 +730,14 @@ __global__ __launch_bounds__(kMxThreads) void attn_join_kernel(const MxAttnParam
 // conversion of each value to fp64 and one or two operations on it there, twice
 // (17 bytes of memory a lane's row), not the reads.
 
-constexpr int kEvictWaves = kMxEvictThreads / 64;
 constexpr int kEvictBatch = 4;    // rows of a lane in flight
-constexpr int kEvictBins = 2 * kMxEvictThreads;
+constexpr int kEvictBins = 2048;
+constexpr int kEvictMaxWaves = kMxEvictThreads / 64;
 
 struct EvictHead {
     uint32_t hist[kEvictBins];
-    uint32_t low[kEvictWaves], high[kEvictWaves];   // smallest and largest key
-    uint32_t count[2][kEvictWaves];
+    uint32_t low[kEvictMaxWaves], high[kEvictMaxWaves];   // smallest and largest key
+    uint32_t count[2][kEvictMaxWaves];
     uint32_t word[4];
     uint32_t cand_key[64], cand_slot[64];
     double mean[256];
@@ -816,6 +818,37 @@ __device__ __forceinline__ void each_value(const GroupRow &r, F f) {
     }
 }
 
+// Whether the sum of a batch's values, channel by channel, is exact in fp32: multiples
+// of half the smallest scale, up to 24 times the largest, are for scales up to 2^16
+// apart (and none so large that the sum is infinite).  Rows of zeros do not count.
+__device__ __forceinline__ bool sum_is_exact(const GroupRow (&r)[kEvictBatch]) {
+    uint32_t low = 255, high = 0;
+#pragma unroll
+    for (int u = 0; u < kEvictBatch; ++u) {
+        const bool zero = (r[u].x[0] | r[u].x[1] | r[u].x[2] | r[u].x[3]) == 0;
+        low = min(low, zero ? 255u : r[u].scale);
+        high = max(high, zero ? 0u : r[u].scale);
+    }
+    return high <= 250 && int(high - low) <= 16;
+}
+__device__ __forceinline__ void add_batch(const GroupRow (&r)[kEvictBatch], double (&sum)[32]) {
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+        auto two = [&](auto sel) {
+            f32x2 v[kEvictBatch];
+#pragma unroll
+            for (int u = 0; u < kEvictBatch; ++u)
+                v[u] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(r[u].x[w], scale_of(r[u].scale), decltype(sel)::value);
+            constexpr int at = decltype(sel)::value;
+            sum[8 * w + 2 * at] += double((v[0][0] + v[1][0]) + (v[2][0] + v[3][0]));
+            sum[8 * w + 2 * at + 1] += double((v[0][1] + v[1][1]) + (v[2][1] + v[3][1]));
+        };
+        two(std::integral_constant<int, 0>()), two(std::integral_constant<int, 1>());
+        two(std::integral_constant<int, 2>()), two(std::integral_constant<int, 3>());
+        __builtin_amdgcn_sched_barrier(0);
+    }
+}
+
 // The boundary of the N highest of n > N keys (equal ones by the lower slot): a
 // row stays if its key is above `key`, or equal to it in a slot up to `slot`.
 // Keys are counted in bins of equal width between the smallest and the largest; the
@@ -825,34 +858,39 @@ struct Boundary {
     uint32_t key;
     int slot;
 };
+template <int THREADS>
 __device__ __forceinline__ Boundary boundary(EvictHead &sh, const uint32_t *keys, int n, int N, uint32_t low, uint32_t high) {
+    constexpr int WAVES = THREADS / 64, EACH = kEvictBins / THREADS;   // bins of a thread
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     int want = N;   // keys to keep among those in [low, high]
     for (;;) {
         const uint32_t range = high - low;
         const int shift = range < uint32_t(kEvictBins) ? 0 : 32 - __builtin_clz(range) - 11;   // (2^11 bins)
-        for (int i = tid; i < kEvictBins; i += kMxEvictThreads) sh.hist[i] = 0;
+        for (int i = tid; i < kEvictBins; i += THREADS) sh.hist[i] = 0;
         __syncthreads();
-        for (int j = tid; j < n; j += kMxEvictThreads) {
+        for (int j = tid; j < n; j += THREADS) {
             const uint32_t at = keys[j] - low;
             if (at <= range) atomicAdd(&sh.hist[at >> shift], 1u);
         }
         __syncthreads();
-        // from the highest bin down, two bins a thread
-        const uint32_t c0 = sh.hist[kEvictBins - 1 - 2 * tid], c1 = sh.hist[kEvictBins - 2 - 2 * tid];
-        uint32_t upto = c0 + c1;
+        // from the highest bin down, a few bins a thread
+        uint32_t c[EACH], mine = 0;
+#pragma unroll
+        for (int i = 0; i < EACH; ++i) mine += c[i] = sh.hist[kEvictBins - 1 - EACH * tid - i];
+        uint32_t upto = mine;
         for (int d = 1; d < 64; d *= 2) {
             const uint32_t o = __shfl_up(upto, d);
             if (lane >= d) upto += o;
         }
         if (lane == 63) sh.count[0][wave] = upto;
         __syncthreads();
-        for (int w = 0; w < kEvictWaves; ++w) upto += w < wave ? sh.count[0][w] : 0u;
-        const uint32_t before = upto - c0 - c1;
-        if (before < uint32_t(want) && before + c0 >= uint32_t(want)) {
-            sh.word[0] = uint32_t(kEvictBins - 1 - 2 * tid), sh.word[1] = before, sh.word[2] = c0;
-        } else if (before + c0 < uint32_t(want) && upto >= uint32_t(want)) {
-            sh.word[0] = uint32_t(kEvictBins - 2 - 2 * tid), sh.word[1] = before + c0, sh.word[2] = c1;
+        for (int w = 0; w < WAVES; ++w) upto += w < wave ? sh.count[0][w] : 0u;
+        uint32_t above = upto - mine;
+#pragma unroll
+        for (int i = 0; i < EACH; ++i) {
+            if (above < uint32_t(want) && above + c[i] >= uint32_t(want))
+                sh.word[0] = uint32_t(kEvictBins - 1 - EACH * tid - i), sh.word[1] = above, sh.word[2] = c[i];
+            above += c[i];
         }
         if (tid == 0) sh.word[3] = 0;
         __syncthreads();
@@ -861,7 +899,7 @@ __device__ __forceinline__ Boundary boundary(EvictHead &sh, const uint32_t *keys
         low += bin << shift;
         high = min(high, low + ((1u << shift) - 1));
         if (count <= 64) {
-            for (int j = tid; j < n; j += kMxEvictThreads) {
+            for (int j = tid; j < n; j += THREADS) {
                 const uint32_t key = keys[j];
                 if (key - low <= high - low) {
                     const uint32_t i = atomicAdd(&sh.word[3], 1u);
@@ -885,7 +923,7 @@ __device__ __forceinline__ Boundary boundary(EvictHead &sh, const uint32_t *keys
         if (shift == 0) break;
     }
     // more than 64 equal keys: the slot of the want-th of them; a wave takes a run of slots
-    const int span = (n + kMxEvictThreads - 1) / kMxEvictThreads * 64;
+    const int span = (n + THREADS - 1) / THREADS * 64;
     const int first = wave * span, last = min(first + span, n);
     int ties = 0;
     for (int base = first; base < last; base += 64)
@@ -893,7 +931,7 @@ __device__ __forceinline__ Boundary boundary(EvictHead &sh, const uint32_t *keys
     if (lane == 0) sh.count[0][wave] = uint32_t(ties);
     __syncthreads();
     int before = 0;
-    for (int w = 0; w < kEvictWaves; ++w) before += w < wave ? int(sh.count[0][w]) : 0;
+    for (int w = 0; w < WAVES; ++w) before += w < wave ? int(sh.count[0][w]) : 0;
     for (int base = first; base < last; base += 64) {
         const bool tie = base + lane < last && keys[min(base + lane, n - 1)] == low;
         const unsigned long long b = __builtin_amdgcn_ballot_w64(tie);
@@ -904,10 +942,10 @@ __device__ __forceinline__ Boundary boundary(EvictHead &sh, const uint32_t *keys
     return {low, int(sh.word[1])};
 }
 
-template <int D, int FORM>
-__global__ __launch_bounds__(kMxEvictThreads) void evict_kernel(const MxEvictParams p) {
-    constexpr int LANES = D / 32;                         // lanes of a row: a group each
-    constexpr int ROWS = kMxEvictThreads / LANES;         // rows that the workgroup takes at a time
+template <int D, int FORM, int THREADS>
+__global__ __launch_bounds__(THREADS, 4) void evict_kernel(const MxEvictParams p) {
+    constexpr int LANES = D / 32, WAVES = THREADS / 64;   // lanes of a row: a group each
+    constexpr int ROWS = THREADS / LANES;         // rows that the workgroup takes at a time
     extern __shared__ __attribute__((aligned(16))) char dyn[];
     __shared__ EvictHead sh;
     uint32_t *keys = reinterpret_cast<uint32_t *>(dyn);
@@ -925,7 +963,7 @@ __global__ __launch_bounds__(kMxEvictThreads) void evict_kernel(const MxEvictPar
     float *scores = p.scores ? p.scores + unit * p.capacity : nullptr;
     uint8_t *keep = p.keep ? p.keep + unit * p.capacity : nullptr;
     if (n <= N && keep)
-        for (int j = tid; j < n; j += kMxEvictThreads) keep[j] = 1;
+        for (int j = tid; j < n; j += THREADS) keep[j] = 1;
     if (n <= N && !scores) return;
     const char *xb = (key_side ? p.c.k : p.c.v) + code_at, *sb = (key_side ? p.c.ks : p.c.vs) + scale_at;
     const int g = tid % LANES, r0 = tid / LANES;
@@ -936,12 +974,22 @@ __global__ __launch_bounds__(kMxEvictThreads) void evict_kernel(const MxEvictPar
     for (int i = 0; i < 32; ++i) mean[i] = 0.0;
     double length = 0.0;
     if (FORM != VD_SCORE_NORM) {
+        bool exact = true;
         for (int j = r0; j < n; j += kEvictBatch * ROWS) {
             load_groups(row, xb, sb, p.c.slot, p.c.sslot, g, j, ROWS, n);
+            exact = exact && sum_is_exact(row);
+            add_batch(row, mean);
+        }
+        if (__builtin_amdgcn_ballot_w64(!exact)) {   // (rare: the wave's rows again, value by value in fp64)
 #pragma unroll
-            for (int u = 0; u < kEvictBatch; ++u) {
-                each_value(row[u], [&](int i, double v) { mean[i] += v; });
-                __builtin_amdgcn_sched_barrier(0);   // one row's conversions at a time: registers
+            for (int i = 0; i < 32; ++i) mean[i] = 0.0;
+            for (int j = r0; j < n; j += kEvictBatch * ROWS) {
+                load_groups(row, xb, sb, p.c.slot, p.c.sslot, g, j, ROWS, n);
+#pragma unroll
+                for (int u = 0; u < kEvictBatch; ++u) {
+                    each_value(row[u], [&](int i, double v) { mean[i] += v; });
+                    __builtin_amdgcn_sched_barrier(0);   // one row's conversions at a time: registers
+                }
             }
         }
         // over the lanes with the same group: halves of the wave and of those keep half
@@ -959,7 +1007,7 @@ __global__ __launch_bounds__(kMxEvictThreads) void evict_kernel(const MxEvictPar
         __syncthreads();
         if (tid < D) {
             double t = 0.0;
-            for (int w = 0; w < kEvictWaves; ++w) t += partial[w * D + tid];
+            for (int w = 0; w < WAVES; ++w) t += partial[w * D + tid];
             sh.mean[tid] = t / double(n);
         }
         __syncthreads();
@@ -1023,27 +1071,27 @@ __global__ __launch_bounds__(kMxEvictThreads) void evict_kernel(const MxEvictPar
     for (int d = 1; d < 64; d *= 2) low = min(low, __shfl_xor(low, d)), high = max(high, __shfl_xor(high, d));
     if (lane == 0) sh.low[wave] = low, sh.high[wave] = high;
     __syncthreads();
-    for (int w = 0; w < kEvictWaves; ++w) low = min(low, sh.low[w]), high = max(high, sh.high[w]);
+    for (int w = 0; w < WAVES; ++w) low = min(low, sh.low[w]), high = max(high, sh.high[w]);
 
     int moved;   // rows to move: movers[k] onto holes[k]
     if (n == N + 1) {
         // the lowest key goes, the highest slot among equal ones
         int gone = -1;
-        for (int j = tid; j < n; j += kMxEvictThreads)
+        for (int j = tid; j < n; j += THREADS)
             if (keys[j] == low) gone = j;
         for (int d = 1; d < 64; d *= 2) gone = max(gone, __shfl_xor(gone, d));
         if (lane == 0) sh.count[0][wave] = uint32_t(gone + 1);
         __syncthreads();
-        for (int w = 0; w < kEvictWaves; ++w) gone = max(gone, int(sh.count[0][w]) - 1);
+        for (int w = 0; w < WAVES; ++w) gone = max(gone, int(sh.count[0][w]) - 1);
         if (keep)
-            for (int j = tid; j < n; j += kMxEvictThreads) keep[j] = j != gone;
+            for (int j = tid; j < n; j += THREADS) keep[j] = j != gone;
         if (tid == 0) holes[0] = uint16_t(gone), movers[0] = uint16_t(N);
         moved = gone < N;
         __syncthreads();
     } else {
-        const Boundary edge = boundary(sh, keys, n, N, low, high);
+        const Boundary edge = boundary<THREADS>(sh, keys, n, N, low, high);
         // the lists in the order of the slots: a wave takes a run of them, counts, then writes
-        const int span = (n + kMxEvictThreads - 1) / kMxEvictThreads * 64;
+        const int span = (n + THREADS - 1) / THREADS * 64;
         const int first = wave * span, last = min(first + span, n);
         const unsigned long long below = (1ull << lane) - 1;
         auto stays = [&](int j) { return keys[j] > edge.key || (keys[j] == edge.key && j <= edge.slot); };
@@ -1059,7 +1107,7 @@ __global__ __launch_bounds__(kMxEvictThreads) void evict_kernel(const MxEvictPar
         __syncthreads();
         int hr = 0, mr = 0;
         nh = nm = 0;
-        for (int w = 0; w < kEvictWaves; ++w) {
+        for (int w = 0; w < WAVES; ++w) {
             hr += w < wave ? int(sh.count[0][w]) : 0;
             mr += w < wave ? int(sh.count[1][w]) : 0;
             nh += int(sh.count[0][w]);
@@ -1079,28 +1127,33 @@ __global__ __launch_bounds__(kMxEvictThreads) void evict_kernel(const MxEvictPar
         __syncthreads();
     }
 
-    // codes in 16-byte words (K's, then V's), scales in one word of D / 32 bytes
+    // The gather: codes in 16-byte words (K's, then V's), a few loads in flight; rows'
+    // scales in one word each, and the tokens' indices.
     constexpr int WORDS = D / 32;
     char *kb = p.c.k + code_at, *vb = p.c.v + code_at, *ksb = p.c.ks + scale_at, *vsb = p.c.vs + scale_at;
-    for (int at = tid; at < moved * 2 * WORDS; at += kMxEvictThreads) {
-        const int i = at / (2 * WORDS), w = at % (2 * WORDS);
-        char *b = w < WORDS ? kb : vb;
-        const uint32_t to = holes[i], from = movers[i];
-        reinterpret_cast<u32x4 *>(b + to * p.c.slot)[w % WORDS] = reinterpret_cast<const u32x4 *>(b + from * p.c.slot)[w % WORDS];
+    int32_t *pos = p.pos ? p.pos + unit * p.capacity : nullptr;
+    using Word = std::conditional_t<D == 64, uint16_t, std::conditional_t<D == 128, uint32_t, u32x2>>;
+    for (int base = tid; base < moved; base += THREADS) {
+        const uint32_t to = holes[base], from = movers[base];
+        const Word a = *reinterpret_cast<const Word *>(ksb + from * p.c.sslot), b = *reinterpret_cast<const Word *>(vsb + from * p.c.sslot);
+        const int32_t t = pos ? pos[from] : 0;
+        *reinterpret_cast<Word *>(ksb + to * p.c.sslot) = a;
+        *reinterpret_cast<Word *>(vsb + to * p.c.sslot) = b;
+        if (pos) pos[to] = t;
     }
-    for (int at = tid; at < moved * 2; at += kMxEvictThreads) {
-        char *b = at & 1 ? vsb : ksb;
-        const uint32_t to = holes[at >> 1], from = movers[at >> 1];
-        if (D == 64)
-            *reinterpret_cast<uint16_t *>(b + to * p.c.sslot) = *reinterpret_cast<const uint16_t *>(b + from * p.c.sslot);
-        else if (D == 128)
-            *reinterpret_cast<uint32_t *>(b + to * p.c.sslot) = *reinterpret_cast<const uint32_t *>(b + from * p.c.sslot);
-        else
-            *reinterpret_cast<u32x2 *>(b + to * p.c.sslot) = *reinterpret_cast<const u32x2 *>(b + from * p.c.sslot);
-    }
-    if (p.pos) {
-        int32_t *pos = p.pos + unit * p.capacity;
-        for (int i = tid; i < moved; i += kMxEvictThreads) pos[holes[i]] = pos[movers[i]];
+    for (int base = tid; base < moved * 2 * WORDS; base += 4 * THREADS) {
+        u32x4 x[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const int at = min(base + u * THREADS, moved * 2 * WORDS - 1), w = at % (2 * WORDS);
+            x[u] = reinterpret_cast<const u32x4 *>((w < WORDS ? kb : vb) + movers[at / (2 * WORDS)] * p.c.slot)[w % WORDS];
+        }
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const int at = base + u * THREADS, w = at % (2 * WORDS);
+            if (at < moved * 2 * WORDS)
+                reinterpret_cast<u32x4 *>((w < WORDS ? kb : vb) + holes[at / (2 * WORDS)] * p.c.slot)[w % WORDS] = x[u];
+        }
     }
 }
 
@@ -1129,13 +1182,13 @@ hipError_t launch_attn(const MxAttnParams &p, int seqs, hipStream_t stream) {
                        dim3((queries + per - 1) / per, p.c.heads, seqs * p.c.layers), kMxThreads, 0, stream, p);
 }
 
-template <int D>
+template <int D, int THREADS>
 hipError_t launch_evict(const MxEvictParams &p, int seqs, size_t lds, hipStream_t stream) {
     const int form = p.variant - (p.variant >= VD_SCORE_KEY_L2 ? VD_SCORE_KEY_L2 : 0);
-    return launch_with(form == VD_SCORE_L2    ? evict_kernel<D, VD_SCORE_L2>
-                       : form == VD_SCORE_DIR ? evict_kernel<D, VD_SCORE_DIR>
-                                              : evict_kernel<D, VD_SCORE_NORM>,
-                       dim3(p.c.heads, p.c.layers, seqs), kMxEvictThreads, lds, stream, p);
+    return launch_with(form == VD_SCORE_L2    ? evict_kernel<D, VD_SCORE_L2, THREADS>
+                       : form == VD_SCORE_DIR ? evict_kernel<D, VD_SCORE_DIR, THREADS>
+                                              : evict_kernel<D, VD_SCORE_NORM, THREADS>,
+                       dim3(p.c.heads, p.c.layers, seqs), THREADS, lds, stream, p);
 }
 
 }  // namespace
@@ -1162,8 +1215,13 @@ hipError_t launch_mx_attention(const MxAttnParams &p, int seqs, int dtype, int D
                       : launch_attn<VD_DTYPE_F32, 256>(p, seqs, stream);
 }
 hipError_t launch_mx_evict(const MxEvictParams &p, int seqs, int D, size_t lds, hipStream_t stream) {
-    return D == 64 ? launch_evict<64>(p, seqs, lds, stream)
-           : D == 128 ? launch_evict<128>(p, seqs, lds, stream) : launch_evict<256>(p, seqs, lds, stream);
+    if (p.threads == kMxEvictThreads)
+        return D == 64    ? launch_evict<64, kMxEvictThreads>(p, seqs, lds, stream)
+               : D == 128 ? launch_evict<128, kMxEvictThreads>(p, seqs, lds, stream)
+                          : launch_evict<256, kMxEvictThreads>(p, seqs, lds, stream);
+    return D == 64    ? launch_evict<64, kMxEvictThreads / 2>(p, seqs, lds, stream)
+           : D == 128 ? launch_evict<128, kMxEvictThreads / 2>(p, seqs, lds, stream)
+                      : launch_evict<256, kMxEvictThreads / 2>(p, seqs, lds, stream);
 }
 
 }  // namespace vd

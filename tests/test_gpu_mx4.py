@@ -391,6 +391,27 @@ def test_evict_ties(variant, n, N):
     _check_evict(cache, before, [n], [N], variant, scores, keep, pos)
 
 
+@pytest.mark.parametrize("variant", ["l2", "dir", "norm"])
+@pytest.mark.parametrize("units", [1, 300])
+@pytest.mark.parametrize("spread,low", [(1, 0), (12, -3), (60, -30), (3, 120), (2, -128)])
+def test_evict_scales_far_apart(variant, units, spread, low):
+    """Rows whose sizes differ by far, the largest and the smallest that the format holds; many units and one."""
+    n, N, D = 90, 60, 64
+    g = torch.Generator().manual_seed(98)
+    size = torch.exp2(torch.randint(low, low + spread, (1, 1, units, n, D // 32, 1), generator=g).double())
+    x = (torch.randn((1, 1, units, n, D // 32, 32), generator=g).double() * size).flatten(-2).clamp(-3.3e38, 3.3e38).float()
+    cache = vd.Mx4Cache.zeros(1, 1, units, n, D, DEV)
+    vd.vd_append_mx4(cache, [0], x.to(DEV), x.to(DEV))
+    before = [y.cpu().clone() for y in cache]
+    pos = torch.arange(n, dtype=torch.int32, device=DEV).repeat(units, 1)
+    scores, keep = torch.full((units, n), -9.0, device=DEV), torch.full((units, n), 7, dtype=torch.uint8, device=DEV)
+    vd.vd_evict_step_mx4(cache, [n], [N], variant, pos=pos, scores_out=scores, keep_out=keep)
+    if low == 120:   # beyond fp32: infinite scores tie
+        assert torch.isfinite(scores).any() and keep.sum(1).eq(N).all()
+        return
+    _check_evict(cache, before, [n], [N], variant, scores, keep, pos)
+
+
 @pytest.mark.parametrize("N", [16383, 8192, 100])
 def test_evict_full_capacity(N):
     """The most slots, in an engine's layout, with and without the optional outputs."""
