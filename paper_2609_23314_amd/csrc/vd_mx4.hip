@@ -969,6 +969,7 @@ __global__ __launch_bounds__(THREADS, 4) void evict_kernel(const MxEvictParams p
     const int g = tid % LANES, r0 = tid / LANES;
 
     GroupRow row[kEvictBatch];
+    load_groups(row, xb, sb, p.c.slot, p.c.sslot, g, r0, ROWS, n);
     double mean[32];
 #pragma unroll
     for (int i = 0; i < 32; ++i) mean[i] = 0.0;
@@ -976,7 +977,7 @@ __global__ __launch_bounds__(THREADS, 4) void evict_kernel(const MxEvictParams p
     if (FORM != VD_SCORE_NORM) {
         bool exact = true;
         for (int j = r0; j < n; j += kEvictBatch * ROWS) {
-            load_groups(row, xb, sb, p.c.slot, p.c.sslot, g, j, ROWS, n);
+            if (j != r0) load_groups(row, xb, sb, p.c.slot, p.c.sslot, g, j, ROWS, n);
             exact = exact && sum_is_exact(row);
             add_batch(row, mean);
         }
@@ -992,6 +993,7 @@ __global__ __launch_bounds__(THREADS, 4) void evict_kernel(const MxEvictParams p
                 }
             }
         }
+        load_groups(row, xb, sb, p.c.slot, p.c.sslot, g, r0, ROWS, n);   // the second reading's first, on their way meanwhile
         // over the lanes with the same group: halves of the wave and of those keep half
         // of the channels each, then the lanes of sixteen are added up
 #pragma unroll
@@ -1027,7 +1029,7 @@ __global__ __launch_bounds__(THREADS, 4) void evict_kernel(const MxEvictParams p
 
     uint32_t low = ~0u, high = 0u;
     for (int j = r0; j < n; j += kEvictBatch * ROWS) {
-        load_groups(row, xb, sb, p.c.slot, p.c.sslot, g, j, ROWS, n);
+        if (j != r0) load_groups(row, xb, sb, p.c.slot, p.c.sslot, g, j, ROWS, n);
         double sq[kEvictBatch], dot[kEvictBatch];
 #pragma unroll
         for (int u = 0; u < kEvictBatch; ++u) {
@@ -1133,26 +1135,29 @@ __global__ __launch_bounds__(THREADS, 4) void evict_kernel(const MxEvictParams p
     char *kb = p.c.k + code_at, *vb = p.c.v + code_at, *ksb = p.c.ks + scale_at, *vsb = p.c.vs + scale_at;
     int32_t *pos = p.pos ? p.pos + unit * p.capacity : nullptr;
     using Word = std::conditional_t<D == 64, uint16_t, std::conditional_t<D == 128, uint32_t, u32x2>>;
-    for (int base = tid; base < moved; base += THREADS) {
-        const uint32_t to = holes[base], from = movers[base];
+    for (int first = 0; first < moved; first += THREADS) {
+        const int rows = min(THREADS, moved - first), mine = first + min(tid, rows - 1);
+        const uint32_t to = holes[mine], from = movers[mine];
         const Word a = *reinterpret_cast<const Word *>(ksb + from * p.c.sslot), b = *reinterpret_cast<const Word *>(vsb + from * p.c.sslot);
         const int32_t t = pos ? pos[from] : 0;
-        *reinterpret_cast<Word *>(ksb + to * p.c.sslot) = a;
-        *reinterpret_cast<Word *>(vsb + to * p.c.sslot) = b;
-        if (pos) pos[to] = t;
-    }
-    for (int base = tid; base < moved * 2 * WORDS; base += 4 * THREADS) {
-        u32x4 x[4];
+        for (int base = tid; base < rows * 2 * WORDS; base += 4 * THREADS) {
+            u32x4 x[4];
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
-            const int at = min(base + u * THREADS, moved * 2 * WORDS - 1), w = at % (2 * WORDS);
-            x[u] = reinterpret_cast<const u32x4 *>((w < WORDS ? kb : vb) + movers[at / (2 * WORDS)] * p.c.slot)[w % WORDS];
+            for (int u = 0; u < 4; ++u) {
+                const int at = min(base + u * THREADS, rows * 2 * WORDS - 1), w = at % (2 * WORDS);
+                x[u] = reinterpret_cast<const u32x4 *>((w < WORDS ? kb : vb) + movers[first + at / (2 * WORDS)] * p.c.slot)[w % WORDS];
+            }
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const int at = base + u * THREADS, w = at % (2 * WORDS);
+                if (at < rows * 2 * WORDS)
+                    reinterpret_cast<u32x4 *>((w < WORDS ? kb : vb) + holes[first + at / (2 * WORDS)] * p.c.slot)[w % WORDS] = x[u];
+            }
         }
-#pragma unroll
-        for (int u = 0; u < 4; ++u) {
-            const int at = base + u * THREADS, w = at % (2 * WORDS);
-            if (at < moved * 2 * WORDS)
-                reinterpret_cast<u32x4 *>((w < WORDS ? kb : vb) + holes[at / (2 * WORDS)] * p.c.slot)[w % WORDS] = x[u];
+        if (tid < rows) {
+            *reinterpret_cast<Word *>(ksb + to * p.c.sslot) = a;
+            *reinterpret_cast<Word *>(vsb + to * p.c.sslot) = b;
+            if (pos) pos[to] = t;
         }
     }
 }
