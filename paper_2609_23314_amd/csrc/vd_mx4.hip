@@ -410,16 +410,26 @@ __global__ __launch_bounds__(kMxThreads) void attn_kernel(const MxAttnParams p) 
 }
 
 // Blocks of query rows.  A workgroup takes 128 query rows of a KV head, a wave 32
-// of them, and passes over the cache 64 rows (32 of D = 256) at a time: the four
-// waves convert a tile of K and V into LDS, while they work on the tile before.
-// With v_mfma_f32_32x32x16_bf16 as above, transposed: a lane holds one query's
-// logits of 16 rows of 32, which are the right operand of the product with V^T.
+// of them, and passes over the cache 64 rows at a time: the four waves bring a tile of
+// K and V into LDS, while they work on the tile before.  As above, transposed: a lane
+// holds one query's logits of 16 rows of 32, which are the right operand of the
+// product with V^T (v_mfma_f32_32x32x16_bf16).
+//
+// K of bf16 queries stays in 4 bits: v_mfma_scale_f32_32x32x64_f8f6f4 takes its codes
+// and scales as they are.  A query is two e4m3 parts with a power of two for each 32
+// channels: eight significant bits, exact but for what is below 2^-21 of the largest
+// of its 32.  That takes the matrix cores the time of the bf16 product, but neither a
+// conversion nor more than a quarter of the LDS reads.  (V's scales belong to rows,
+// along which its product sums: it is converted.)  fp32 queries meet K in bf16.
 
 constexpr int kBlockRows = 64;
-template <int D>
-constexpr int kKStride = D * 2 + 16;   // sixteen rows' 16-byte reads fall into different banks
-template <int D>
-constexpr int kBlockBytes = kBlockRows * (kKStride<D> + D * 2);   // K's tile, then V's
+template <int DTYPE, int D>
+struct KTile {   // K in LDS; sixteen rows' 16-byte reads fall into different banks
+    static constexpr bool CODES = DTYPE == VD_DTYPE_BF16;
+    static constexpr int STRIDE = (CODES ? D / 2 : D * 2) + 16;
+    static constexpr int SCALE = D == 256 ? 8 : 4;                                  // bytes of a row's scales
+    static constexpr int BYTES = kBlockRows * (STRIDE + (CODES ? SCALE : 0));       // (behind all rows)
+};
 
 // V's tile has no padding: where four rows are read together 64 bytes wide, and
 // sixteen lanes write 16 bytes each, both meet every bank once if a row's 64-byte
@@ -432,7 +442,7 @@ __device__ __forceinline__ int v_place(int row, int unit, int piece) {
 
 // A thread's part of a tile on its way from memory: groups of K, then groups of V
 // (of D = 64 one group of either).
-template <int D>
+template <int DTYPE, int D>
 struct BlockStage {
     static constexpr int GROUPS = D / 32, ROWS = kBlockRows, ITEMS = 2 * ROWS * GROUPS / kMxThreads, K_ITEMS = (ITEMS + 1) / 2;
     u32x4 x[ITEMS];
@@ -456,29 +466,129 @@ struct BlockStage {
         }
     }
     __device__ __forceinline__ void store(int i, char *kt, char *vt) const {
-            const int row = at(i) / GROUPS, group = at(i) % GROUPS;
-            uint32_t byte;
-            if (is_v(i)) {
-                byte = i < K_ITEMS ? vs[i % K_ITEMS].byte(group) : vbyte[i];
-                byte = byte == 255u ? 0u : byte;
-            } else {
-                byte = ks[i % K_ITEMS].byte(group) | ks[i % K_ITEMS].nan_bits() | vs[i % K_ITEMS].nan_bits();
-            }
+        using Tile = KTile<DTYPE, D>;
+        const int row = at(i) / GROUPS, group = at(i) % GROUPS;
+        if (is_v(i)) {
+            const uint32_t own = i < K_ITEMS ? vs[i % K_ITEMS].byte(group) : vbyte[i], byte = own == 255u ? 0u : own;
 #pragma unroll
-            for (int w = 0; w < 4; ++w)
-                *reinterpret_cast<bf16x8 *>(is_v(i) ? vt + v_place<D>(row, group, w) : kt + row * kKStride<D> + group * 64 + 16 * w) =
-                    decode8(x[i][w], scale_of(byte));
+            for (int w = 0; w < 4; ++w) *reinterpret_cast<bf16x8 *>(vt + v_place<D>(row, group, w)) = decode8(x[i][w], scale_of(byte));
+            return;
+        }
+        const uint32_t nan = ks[i % K_ITEMS].nan_bits() | vs[i % K_ITEMS].nan_bits();
+        if (Tile::CODES) {
+            *reinterpret_cast<u32x4 *>(kt + row * Tile::STRIDE + group * 16) = x[i];
+            kt[kBlockRows * Tile::STRIDE + row * Tile::SCALE + group] = char(ks[i % K_ITEMS].byte(group) | nan);
+            return;
+        }
+        const uint32_t byte = ks[i % K_ITEMS].byte(group) | nan;
+#pragma unroll
+        for (int w = 0; w < 4; ++w)
+            *reinterpret_cast<bf16x8 *>(kt + row * Tile::STRIDE + group * 64 + 16 * w) = decode8(x[i][w], scale_of(byte));
     }
 };
 
 __device__ __forceinline__ float dot2(bf16x2 a, bf16x2 b, float c) { return __builtin_amdgcn_fdot2_f32_bf16(a, b, c, false); }
 typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef int i32x8 __attribute__((ext_vector_type(8)));
+
+// A wave's 32 queries as right operands, and their logits with a tile of K: a lane
+// has query c = lane & 31, rows 32 t + 8 (r / 4) + 4 half + r % 4.
+template <int DTYPE, int D>
+struct BlockQueries {   // fp32: three bf16 parts, channels 16 f + 8 half + e
+    static constexpr int FRAGS = D / 16, QP = 3, PRODUCTS = FRAGS * QP;
+    bf16x8 q[QP][FRAGS];
+    __device__ __forceinline__ void load(const char *src, int half, uint32_t flip) {
+#pragma unroll
+        for (int f = 0; f < FRAGS; ++f) load_query<DTYPE, QP>(q, f, src, 16 * f + 8 * half, flip);
+    }
+    __device__ __forceinline__ f32x16 logits(const char *kt, int t, int c, int half) const {
+        f32x16 z = {};
+#pragma unroll
+        for (int f = 0; f < FRAGS; ++f) {
+            const bf16x8 a = *reinterpret_cast<const bf16x8 *>(kt + (32 * t + c) * KTile<DTYPE, D>::STRIDE + (16 * f + 8 * half) * 2);
+#pragma unroll
+            for (int part = QP - 1; part >= 0; --part) z = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, q[part][f], z, 0, 0, 0);
+        }
+        return z;
+    }
+};
+
+// The product of 64 channels: codes and their scale (byte BYTE of ka), e4m3 values and theirs.
+template <int BYTE, int PART>
+__device__ __forceinline__ f32x16 mx_product(const u32x4 &k, uint32_t ks, const i32x8 &q, uint32_t qs, const f32x16 &z) {
+    const i32x8 a = {int(k[0]), int(k[1]), int(k[2]), int(k[3]), 0, 0, 0, 0};
+    return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, q, z, 4, 0, BYTE, int(ks), BYTE + PART, int(qs));
+}
+
+template <int D>
+struct BlockQueries<VD_DTYPE_BF16, D> {
+    // For 64 channels the left operand has a half's lanes hold 32 neighbouring ones (a
+    // group), the right one 16 of the first 32 and 16 of the second; scales are a half's own.
+    static constexpr int FRAGS = D / 64, PRODUCTS = FRAGS * 2;
+    i32x8 high[FRAGS], low[FRAGS];
+    uint32_t scale[(FRAGS + 1) / 2];   // bytes: of high and low of an even f, then of an odd one
+    __device__ __forceinline__ void load(const char *src, int half, uint32_t flip) {
+#pragma unroll
+        for (int f = 0; f < FRAGS; ++f) {
+            uint32_t byte[2];
+#pragma unroll
+            for (int b = 0; b < 2; ++b) {
+                u32x4 x[2];
+#pragma unroll
+                for (int w = 0; w < 2; ++w)
+                    x[w] = *reinterpret_cast<const u32x4 *>(src + (64 * f + 32 * b + 16 * half + 8 * w) * 2) ^ (flip | flip >> 16);
+                uint32_t most = 0;
+#pragma unroll
+                for (int w = 0; w < 8; ++w) most = max(most, max(x[w >> 2][w & 3] & 0x7FFF0000u, x[w >> 2][w & 3] << 16 & 0x7FFF0000u));
+                most = max(most, uint32_t(__shfl_xor(int(most), 32)));
+                // 2^(byte - 127): the largest becomes 128 .. 256, e4m3 ends at 448
+                byte[b] = uint32_t(max(int(most >> 23) - 7, 4));
+                const float to = as_float((254u - byte[b]) << 23);
+#pragma unroll
+                for (int w = 0; w < 4; ++w) {   // four channels
+                    const uint32_t u = x[w >> 1][2 * (w & 1)], v = x[w >> 1][2 * (w & 1) + 1];
+                    const float y[4] = {as_float(u << 16) * to, as_float(u & 0xFFFF0000u) * to, as_float(v << 16) * to,
+                                        as_float(v & 0xFFFF0000u) * to};
+                    int h = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false);
+                    h = __builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], h, true);
+                    const float r0 = y[0] - __builtin_amdgcn_cvt_f32_fp8(h, 0), r1 = y[1] - __builtin_amdgcn_cvt_f32_fp8(h, 1);
+                    const float r2 = y[2] - __builtin_amdgcn_cvt_f32_fp8(h, 2), r3 = y[3] - __builtin_amdgcn_cvt_f32_fp8(h, 3);
+                    int l = __builtin_amdgcn_cvt_pk_fp8_f32(r0 * 16.0f, r1 * 16.0f, 0, false);
+                    l = __builtin_amdgcn_cvt_pk_fp8_f32(r2 * 16.0f, r3 * 16.0f, l, true);
+                    high[f][4 * b + w] = h;
+                    low[f][4 * b + w] = l;
+                }
+            }
+            const uint32_t own = half ? byte[1] : byte[0], both = own | (own - 4) << 8;
+            scale[f / 2] = f % 2 ? scale[f / 2] | both << 16 : both;
+        }
+    }
+    __device__ __forceinline__ f32x16 logits(const char *kt, int t, int c, int half) const {
+        using Tile = KTile<VD_DTYPE_BF16, D>;
+        const char *row = kt + (32 * t + c) * Tile::STRIDE + 16 * half;
+        const uint32_t *scales = reinterpret_cast<const uint32_t *>(kt + kBlockRows * Tile::STRIDE + (32 * t + c) * Tile::SCALE);
+        f32x16 z = {};
+#pragma unroll
+        for (int f = 0; f < FRAGS; f += 2) {
+            const uint32_t ks = scales[f / 2] >> (8 * half);
+            const u32x4 k = *reinterpret_cast<const u32x4 *>(row + 32 * f);
+            z = mx_product<0, 1>(k, ks, low[f], scale[f / 2], z);
+            z = mx_product<0, 0>(k, ks, high[f], scale[f / 2], z);
+            if (FRAGS > 1) {
+                const u32x4 next = *reinterpret_cast<const u32x4 *>(row + 32 * (f + 1));
+                z = mx_product<2, 1>(next, ks, low[(f + 1) % FRAGS], scale[f / 2], z);
+                z = mx_product<2, 0>(next, ks, high[(f + 1) % FRAGS], scale[f / 2], z);
+            }
+        }
+        return z;
+    }
+};
 
 template <int DTYPE, int D>
 __global__ __launch_bounds__(kMxThreads, block_groups(DTYPE, D)) void attn_block_kernel(const MxAttnParams p) {
-    constexpr int FRAGS = D / 16, CT = D / 32, SUBS = kBlockRows / 32;
-    constexpr int QP = DTYPE == VD_DTYPE_F32 ? 3 : 1, PP = DTYPE == VD_DTYPE_F32 ? 2 : 1;
-    __shared__ __attribute__((aligned(16))) char lds[2 * kBlockBytes<D>];
+    constexpr int CT = D / 32, SUBS = kBlockRows / 32, PP = DTYPE == VD_DTYPE_F32 ? 2 : 1;
+    constexpr int T = kBlockRows, KT = KTile<DTYPE, D>::BYTES, VT = T * D * 2, STEPS = SUBS * 2;
+    __shared__ __attribute__((aligned(16))) char lds[2 * (KT + VT)];
     const int split = blockIdx.x / p.tiles, tile = blockIdx.x % p.tiles;
     const int head = blockIdx.y, s = blockIdx.z / p.c.layers, layer = blockIdx.z % p.c.layers;
     const int n = p.n[s], rows = p.rows[s], G = p.group;
@@ -486,7 +596,6 @@ __global__ __launch_bounds__(kMxThreads, block_groups(DTYPE, D)) void attn_block
     if (m0 >= queries) return;
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, c = lane & 31, half = lane >> 5;
     const int seen = max(0, n - rows + 1 + min(m0 + kMxBlockTile - 1, queries - 1) / G);
-    constexpr int T = kBlockRows;
     const int share = ((seen + p.splits - 1) / p.splits + T - 1) / T * T;
     const int begin = min(split * share, seen), end = min(begin + share, seen);
     const int wm0 = m0 + 32 * wave, m = wm0 + c;
@@ -494,12 +603,8 @@ __global__ __launch_bounds__(kMxThreads, block_groups(DTYPE, D)) void attn_block
     const int limit = min(n - rows + 1 + i, end);
     const int all_see = min(n - rows + 1 + min(wm0, queries - 1) / G, end);   // rows that every query of the wave sees
 
-    bf16x8 q[QP][FRAGS];   // channels 16 f + 8 half + e of query c
-    {
-        const char *src = p.q + s * p.qs[0] + layer * p.qs[1] + (head * G + g) * p.qs[2] + i * p.qs[3];
-#pragma unroll
-        for (int f = 0; f < FRAGS; ++f) load_query<DTYPE, QP>(q, f, src, 16 * f + 8 * half, p.flip);
-    }
+    BlockQueries<DTYPE, D> query;
+    query.load(p.q + s * p.qs[0] + layer * p.qs[1] + (head * G + g) * p.qs[2] + i * p.qs[3], half, p.flip);
     const char *kb = p.c.k + s * p.c.seq + layer * p.c.layer + head * p.c.head;
     const char *vb = p.c.v + s * p.c.seq + layer * p.c.layer + head * p.c.head;
     const char *ksb = p.c.ks + s * p.c.sseq + layer * p.c.slayer + head * p.c.shead;
@@ -519,21 +624,6 @@ __global__ __launch_bounds__(kMxThreads, block_groups(DTYPE, D)) void attn_block
     for (int ct = 0; ct < (CT < 4 ? CT : 4); ++ct)
         v_at[ct] = v_place<D>(4 * half + ((lane & 15) >> 2), ct, 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) + (lane & 1) * 8;
 
-    // logits of a tile: a lane has query c, rows 32 t + 8 (r / 4) + 4 half + r % 4
-    auto logits = [&](f32x16 (&z)[SUBS], const char *kt) {
-#pragma unroll
-        for (int t = 0; t < SUBS; ++t) {
-#pragma unroll
-            for (int r = 0; r < 16; ++r) z[t][r] = 0.0f;
-#pragma unroll
-            for (int f = 0; f < FRAGS; ++f) {
-                const bf16x8 a = *reinterpret_cast<const bf16x8 *>(kt + (32 * t + c) * kKStride<D> + (16 * f + 8 * half) * 2);
-#pragma unroll
-                for (int part = QP - 1; part >= 0; --part)
-                    z[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, q[part][f], z[t], 0, 0, 0);
-            }
-        }
-    };
     // weights of sixteen rows: the right operand of the product with V
     auto weights = [&](bf16x8 (&w)[PP], const f32x16 &z, int k) {
 #pragma unroll
@@ -563,10 +653,9 @@ __global__ __launch_bounds__(kMxThreads, block_groups(DTYPE, D)) void attn_block
             a[ct] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
         }
     };
-    constexpr int KT = T * kKStride<D>, VT = T * D * 2, STEPS = SUBS * 2;
-    constexpr int ITEMS = BlockStage<D>::ITEMS;
+    constexpr int ITEMS = BlockStage<DTYPE, D>::ITEMS;
     char *k_lds = lds, *v_lds = lds + 2 * KT;
-    BlockStage<D> stage;
+    BlockStage<DTYPE, D> stage;
     if (begin < end) {
         stage.load(kb, vb, ksb, vsb, p.c.slot, p.c.sslot, begin, begin, end);
 #pragma unroll
@@ -578,15 +667,16 @@ __global__ __launch_bounds__(kMxThreads, block_groups(DTYPE, D)) void attn_block
         stage.load(kb, vb, ksb, vsb, p.c.slot, p.c.sslot, j0 + T, j0 + T, end);   // (behind the last tile: not used)
         const char *vt = v_lds + buffer * VT;
         f32x16 now[SUBS];
-        logits(now, k_lds + buffer * KT);
+#pragma unroll
+        for (int t = 0; t < SUBS; ++t) now[t] = query.logits(k_lds + buffer * KT, t, c, half);
         bf16x8 va[2][CT], w[2][PP];
         read_values(va[0], vt, 0);
         // the next tile's loads first, and the matrix cores' operands read well ahead of the products
         __builtin_amdgcn_sched_group_barrier(0x020, 16, 0);
         __builtin_amdgcn_sched_group_barrier(0x100, 8, 0);
 #pragma unroll
-        for (int i = 0; i < SUBS * FRAGS; ++i) {
-            __builtin_amdgcn_sched_group_barrier(0x008, QP, 0);
+        for (int i = 0; i < SUBS * BlockQueries<DTYPE, D>::FRAGS; ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x008, BlockQueries<DTYPE, D>::PRODUCTS / BlockQueries<DTYPE, D>::FRAGS, 0);
             __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
         }
         if (j0 + T > all_see) {

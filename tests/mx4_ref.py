@@ -35,16 +35,21 @@ def decode(codes, scales):
 
 def attention(k, v, q, n, rows, scale):
     """One unit's output [G, t, D] of queries [G, t, D] over values [C, D], with
-    the weighted mean of |v| and the largest sum |q_c k_c| of each query row."""
+    the weighted mean of |v| and, over the cached rows that a query row sees, the
+    largest sum |q_c k_c| and the largest sum of |k_c| times the largest |q| of c's
+    32 channels."""
     G, t, D = q.shape
-    out, size, prod = torch.zeros((G, t, D)).double(), torch.zeros((G, t, D)).double(), torch.zeros((G, t, 1)).double()
+    out, size = torch.zeros((G, t, D)).double(), torch.zeros((G, t, D)).double()
+    prod, most = torch.zeros((G, t, 1)).double(), torch.zeros((G, t, 1)).double()
+    top = q.abs().unflatten(-1, (-1, 32)).amax(-1).repeat_interleave(32, -1)
     for i in range(rows):
         m = max(0, n - rows + 1 + i)
         if m:
             w = torch.softmax(q[:, i] @ k[:m].T * scale, -1)
             out[:, i], size[:, i] = w @ v[:m], w @ v[:m].abs()
             prod[:, i, 0] = (q[:, i].abs() @ k[:m].abs().T).amax(-1)
-    return out, size, prod
+            most[:, i, 0] = (top[:, i] @ k[:m].abs().T).amax(-1)
+    return out, size, prod, most
 
 
 def scores(x, variant):
