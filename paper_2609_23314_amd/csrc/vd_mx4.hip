@@ -281,9 +281,9 @@ __global__ __launch_bounds__(kMxThreads) void attn_kernel(const MxAttnParams p) 
     const bf16x8 ones = __builtin_bit_cast(bf16x8, (u32x4{one2, one2, one2, one2}));
     float top = -INFINITY, sub = 0.0f;   // the maximum that the weights are relative to
 
-    for (int j0 = begin + 32 * wave; j0 < end; j0 += 128) {
-        Quarter<D> kc[2], vc[2];
-        Scales<D> ks[2], vs[2];
+    Quarter<D> kc[2], vc[2];
+    Scales<D> ks[2], vs[2];
+    auto load = [&](int j0) {
 #pragma unroll
         for (int t = 0; t < 2; ++t) {   // rows behind the end: the last row again, hidden below
             const uint32_t row = uint32_t(min(j0 + 16 * t + c, end - 1));
@@ -292,6 +292,9 @@ __global__ __launch_bounds__(kMxThreads) void attn_kernel(const MxAttnParams p) 
             vc[t] = load_quarter<D>(vb + row * p.c.slot, kq);
             vs[t] = load_scales<D>(vsb + row * p.c.sslot);
         }
+    };
+    if (begin + 32 * wave < end) load(begin + 32 * wave);
+    for (int j0 = begin + 32 * wave; j0 < end; j0 += 128) {
         f32x4 z[2];
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
@@ -310,6 +313,7 @@ __global__ __launch_bounds__(kMxThreads) void attn_kernel(const MxAttnParams p) 
                 *reinterpret_cast<bf16x8 *>(tile_lds + (16 * t + c) * kVStride<D> + (kq * (D / 4) + 8 * f) * 2) = decode8(vc[t].w[f], vscale);
             }
         }
+        load(j0 + 128);   // on its way while this one's weights are made (behind the end: not used)
         // lane: query c, rows j0 + 16 t + 4 kq + r
         if (j0 + 32 > min(all_see, end)) {
 #pragma unroll
@@ -766,13 +770,21 @@ __global__ __launch_bounds__(kMxThreads) void attn_join_kernel(const MxAttnParam
     if (query < 0) return;                                                         // (a sequence without query rows)
     const int64_t unit = (int64_t(s) * p.c.layers + layer) * p.c.heads + head;
     const int64_t all = int64_t(p.max_rows) * G, first = unit * p.splits * all + query;
+    const int mine = at / LANES, ch = at % LANES * 4;
+    f32x4 x[4], o = {0, 0, 0, 0};
+    auto load = [&](int base) {   // (behind the last split: the last again, not added)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            x[i] = *reinterpret_cast<const f32x4 *>(p.ws_acc + (first + min(base + i * AT_ONCE + mine, p.splits - 1) * all) * D + ch);
+    };
+    load(0);
     float top[2], sum[2], high = -INFINITY;
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-        const bool mine = lane + 64 * i < p.splits;
-        const float *ml = p.ws_ml + (first + (mine ? lane + 64 * i : 0) * all) * 2;
-        top[i] = mine ? ml[0] : -INFINITY;
-        sum[i] = mine ? ml[1] : 0.0f;
+        const bool has = lane + 64 * i < p.splits;
+        const float *ml = p.ws_ml + (first + (has ? lane + 64 * i : 0) * all) * 2;
+        top[i] = has ? ml[0] : -INFINITY;
+        sum[i] = has ? ml[1] : 0.0f;
         high = fmaxf(high, top[i]);
     }
     for (int d = 1; d < 64; d *= 2) high = fmaxf(high, __shfl_xor(high, d));
@@ -783,14 +795,15 @@ __global__ __launch_bounds__(kMxThreads) void attn_join_kernel(const MxAttnParam
         total = fmaf(sum[i], top[i], total);
     }
     for (int d = 1; d < 64; d *= 2) total += __shfl_xor(total, d);
-    f32x4 o = {0, 0, 0, 0};
-    const int mine = at / LANES, ch = at % LANES * 4;
-    for (int base = 0; base < p.splits; base += AT_ONCE) {
-        const int split = min(base + mine, p.splits - 1);
-        const float f0 = __shfl(top[0], split & 63), f1 = __shfl(top[1], split & 63), f = split < 64 ? f0 : f1;
-        const f32x4 x = *reinterpret_cast<const f32x4 *>(p.ws_acc + (first + split * all) * D + ch);
-        if (base + mine < p.splits)
-            for (int e = 0; e < 4; ++e) o[e] = fmaf(x[e], f, o[e]);
+    for (int base = 0; base < p.splits; base += 4 * AT_ONCE) {
+        if (base > 0) load(base);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int split = base + i * AT_ONCE + mine;
+            const float f0 = __shfl(top[0], split & 63), f1 = __shfl(top[1], split & 63), f = split < 64 ? f0 : f1;
+            if (split < p.splits)
+                for (int e = 0; e < 4; ++e) o[e] = fmaf(x[i][e], f, o[e]);
+        }
     }
     if (AT_ONCE > 1) {
         sums[threadIdx.x] = o;
