@@ -186,8 +186,8 @@ size_t attn_ws(const vd_mx4_cache *c, int64_t max_rows, const AttnPlan &a) {
 }
 vd_status check_queries(const vd_mx4_cache *c, int32_t dtype, int32_t max_rows) {
     if (!known_dtype(dtype) || max_rows < 1) return VD_ERR_INVALID_ARG;
-    // query rows of a unit and workgroups of a launch, in 32 bits
-    if (int64_t(max_rows) * (c->num_q_heads / c->num_kv_heads) > INT32_MAX / vd::kMxMaxSplits / 256) return VD_ERR_UNSUPPORTED;
+    // query rows of a unit, and threads of a launch along a grid's first axis, in 32 bits
+    if (int64_t(max_rows) * (c->num_q_heads / c->num_kv_heads) > (1 << 26)) return VD_ERR_UNSUPPORTED;
     return VD_OK;
 }
 
@@ -362,10 +362,15 @@ extern "C" vd_status vd_qk_norm_rope(const vd_rope_args *a, vd_stream stream) {
     if (heads > INT32_MAX / a->num_layers || tokens > INT32_MAX / 2) return VD_ERR_UNSUPPORTED;
     const int64_t all = heads * a->num_layers, lanes = a->head_dim / 8;
     // Rows of a token that one group of lanes takes, whose cos and sin it makes once:
-    // as many as leave about sixteen waves for each CU, sixteen at most.
+    // about 4 KB of them, read and written, but only as many as leave about sixteen waves
+    // for each CU.  More make the groups' paths through memory long and scattered (us, rows
+    // 1, 2, 4, 8, 16: 512 tokens x 1280 rows of 128 bf16 channels 111, 84, 73, 71, 78; 999
+    // tokens x 156 of 256 fp32 channels 60, 62, 67, 69, 68).
     const int64_t groups = int64_t(256) * 16 * 64 / lanes;
+    const int64_t bytes = a->head_dim * (elem_bytes(a->dtype) + elem_bytes(a->q.x ? a->q.out_dtype : a->k.out_dtype));
+    const int64_t most = std::max<int64_t>(1, 4096 / bytes);
     p.tokens = int32_t(tokens);
-    p.per_item = int32_t(std::max<int64_t>(1, std::min<int64_t>(16, tokens * all / groups)));
+    p.per_item = int32_t(std::max<int64_t>(1, std::min<int64_t>(most, tokens * all / groups)));
     p.items = int32_t((all + p.per_item - 1) / p.per_item);
     if (tokens * p.items > INT32_MAX) return VD_ERR_UNSUPPORTED;
     return launched(vd::launch_rope(p, a->dtype, a->head_dim, a->interleaved != 0, reinterpret_cast<hipStream_t>(stream)));

@@ -275,11 +275,28 @@ def test_attention_scales(scale, dtype, t):
     _check_attention(cache, q, [130], [t], vd.vd_attention_mx4(cache, q, [130], scale=scale), scale)
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("t", [1, 70])
+@pytest.mark.parametrize("size,spread", [(-90, 0), (60, 0), (-10, 20), (-90, 8)])
+def test_attention_query_sizes(dtype, t, size, spread):
+    """Very small and very large queries, and channels whose sizes differ by far (a
+    bf16 query's parts hold them relative to the largest of 32); zeros among them."""
+    D = 128
+    g = torch.Generator().manual_seed(69)
+    cache = _cache(1, 1, 1, 200, D, 70)
+    by = torch.exp2(size + torch.randint(0, spread + 1, (D,), generator=g).float())
+    q = (torch.randn((1, 1, 2, t, D), generator=g) * by).to(dtype)
+    q[..., 32:64] = 0
+    scale = 2.0 ** (-size - spread) * 0.05
+    out = vd.vd_attention_mx4(cache, q.to(DEV), [200], scale=scale)
+    _check_attention(cache, q, [200], [t], out, scale)
+
+
 def test_attention_nonfinite_queries():
     """A query row with NaN or an infinity spoils its own output alone."""
     cache = _cache(1, 1, 1, 200, 128, 65)
     for dtype in (torch.bfloat16, torch.float32):
-        for t in (3, 30):
+        for t in (3, 30, 90):
             q = _rows((1, 1, 2, t, 128), dtype, 66, 0.3).to(DEV)
             clean = vd.vd_attention_mx4(cache, q, [200])
             for x in (math.nan, math.inf):
