@@ -1069,7 +1069,8 @@ __global__ __launch_bounds__(THREADS, 4) void evict_kernel(const MxEvictParams p
         for (int j = tid; j < n; j += THREADS) keep[j] = 1;
     if (n <= N && !scores) return;
     const char *xb = (key_side ? p.c.k : p.c.v) + code_at, *sb = (key_side ? p.c.ks : p.c.vs) + scale_at;
-    const int g = tid % LANES, r0 = tid / LANES;
+    const int g = tid % LANES, r0 = tid / LANES;          // the lane's group, its row of the workgroup's
+    const int w0 = __builtin_amdgcn_readfirstlane(r0);     // the wave's first
 
     GroupRow row[kEvictBatch];
     load_groups(row, xb, sb, p.c.slot, p.c.sslot, g, r0, ROWS, n);
@@ -1079,10 +1080,17 @@ __global__ __launch_bounds__(THREADS, 4) void evict_kernel(const MxEvictParams p
     double length = 0.0;
     if (FORM != VD_SCORE_NORM) {
         bool exact = true;
-        for (int j = r0; j < n; j += kEvictBatch * ROWS) {
-            if (j != r0) load_groups(row, xb, sb, p.c.slot, p.c.sslot, g, j, ROWS, n);
+        int from = 0;
+        for (; from + w0 + (kEvictBatch - 1) * ROWS < n; from += kEvictBatch * ROWS) {
+            if (from > 0) load_groups(row, xb, sb, p.c.slot, p.c.sslot, g, from + r0, ROWS, n);
             exact = exact && sum_is_exact(row);
             add_batch(row, mean);
+        }
+        if (from + w0 < n) {   // the rest, a row at a time
+            if (from > 0) load_groups(row, xb, sb, p.c.slot, p.c.sslot, g, from + r0, ROWS, n);
+#pragma unroll
+            for (int u = 0; u + 1 < kEvictBatch; ++u)
+                if (from + w0 + u * ROWS < n) each_value(row[u], [&](int i, double v) { mean[i] += v; });
         }
         if (__builtin_amdgcn_ballot_w64(!exact)) {   // (rare: the wave's rows again, value by value in fp64)
 #pragma unroll
@@ -1137,11 +1145,12 @@ __global__ __launch_bounds__(THREADS, 4) void evict_kernel(const MxEvictParams p
 #pragma unroll
         for (int u = 0; u < kEvictBatch; ++u) {
             double a = 0.0, b = 0.0;
-            each_value(row[u], [&](int i, double v) {
-                if (FORM == VD_SCORE_L2) v -= mean[i];
-                a = fma(v, v, a);
-                if (FORM == VD_SCORE_DIR) b = fma(v, mean[i], b);
-            });
+            if (j - r0 + w0 + u * ROWS < n)   // (else none of the wave's rows)
+                each_value(row[u], [&](int i, double v) {
+                    if (FORM == VD_SCORE_L2) v -= mean[i];
+                    a = fma(v, v, a);
+                    if (FORM == VD_SCORE_DIR) b = fma(v, mean[i], b);
+                });
             sq[u] = row_sum<LANES>(a);
             if (FORM == VD_SCORE_DIR) dot[u] = row_sum<LANES>(b);
             __builtin_amdgcn_sched_barrier(0);
