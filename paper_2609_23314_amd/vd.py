@@ -11,6 +11,7 @@ kv_head, head_dim]`` cache is ``x.permute(0, 2, 1, 3).unsqueeze(1)``).
 Per-unit arrays are ``[seq, layer, kv_head, ...]`` contiguous, i.e. unit
 ``u = (s * layers + l) * kv_heads + h``.
 """
+import array
 import contextlib
 import ctypes
 import os
@@ -497,8 +498,8 @@ class Mx4Cache(NamedTuple):
 
 
 # As above: what every call goes through keeps to few and plain Python steps (the host's
-# time for sixteen sequences' append and read-back 31 -> 26 us, for one layer's attention
-# 18 -> 15, where the GPU takes 7 and 18).
+# time for sixteen sequences' append and read-back 31 -> 24 us, for one layer's attention
+# 18 -> 14, where the GPU takes 7 and 18).
 
 def mx4_desc(cache, num_q_heads=None) -> VdMx4Cache:
     """Descriptor of an ``Mx4Cache``."""
@@ -537,15 +538,18 @@ def _rows_view(x, name, shape, dtype, dev):
 
 
 def _host_list(x, S, name):
-    """``_host_i32`` for what mostly is a list of S ints."""
-    if type(x) is list and len(x) == S and max(x) < 2 ** 31 and min(x) >= -2 ** 31:
+    """``_host_i32`` for what mostly is a list of S ints; and its address."""
+    if type(x) is list and len(x) == S:
         try:
-            return (ctypes.c_int32 * S)(*x)
-        except TypeError:
+            made = array.array("i", x)   # (checks types and range)
+            return made, made.buffer_info()[0]
+        except (TypeError, OverflowError):
             pass
-    return _host_i32(x, S, name)
+    made = _host_i32(x, S, name)
+    return made, _ptr(made)
 
 
+_no_list = (None, None)
 _nothing = contextlib.nullcontext()
 
 
@@ -582,12 +586,12 @@ def vd_append_mx4(cache, n_old, k_rows, v_rows, rows=None, pos=None, pos0=None, 
     vp, vs = _rows_view(v_rows, "v_rows", shape, dtype, dev)
     if pos is not None:
         _need(pos, "pos", torch.int32, S * L * H * C, dev)
-    n_h = _host_list(n_old, S, "n_old")
-    r_h = None if rows is None else _host_list(rows, S, "rows")
-    p_h = None if pos0 is None else _host_list(pos0, S, "pos0")
+    n_h, n_p = _host_list(n_old, S, "n_old")
+    r_h, r_p = _no_list if rows is None else _host_list(rows, S, "rows")
+    p_h, p_p = _no_list if pos0 is None else _host_list(pos0, S, "pos0")
     with _on(dev, stream):
         _check("vd_append_mx4", load().vd_append_mx4(
-            ctypes.byref(desc), _ptr(n_h), _ptr(r_h), t, _dtype_code(k_rows), kp, ks, vp, vs, _ptr(pos), _ptr(p_h),
+            ctypes.byref(desc), n_p, r_p, t, _dtype_code(k_rows), kp, ks, vp, vs, _ptr(pos), p_p,
             _stream(dev, stream)))
     if pos is None:
         _moved(*cache)
@@ -603,8 +607,8 @@ def vd_read_mx4(cache, first, t, rows=None, k_out=None, v_out=None, *, dtype=tor
     S, L, H, _, B = cache[0].shape
     dev, t = cache[0].device, int(t)
     shape = (S, L, H, t, 2 * B)
-    n_h = _host_list(first, S, "first")
-    r_h = None if rows is None else _host_list(rows, S, "rows")
+    n_h, n_p = _host_list(first, S, "first")
+    r_h, r_p = _no_list if rows is None else _host_list(rows, S, "rows")
     with _on(dev, stream):
         if k_out is None:
             k_out = torch.empty(shape, dtype=dtype, device=dev)
@@ -614,7 +618,7 @@ def vd_read_mx4(cache, first, t, rows=None, k_out=None, v_out=None, *, dtype=tor
             _no_grad("vd_read_mx4")
         kp, ks = _rows_view(k_out, "k_out", shape, k_out.dtype, dev)
         vp, vs = _rows_view(v_out, "v_out", shape, k_out.dtype, dev)
-        _check("vd_read_mx4", load().vd_read_mx4(ctypes.byref(desc), _ptr(n_h), _ptr(r_h), t, _dtype_code(k_out),
+        _check("vd_read_mx4", load().vd_read_mx4(ctypes.byref(desc), n_p, r_p, t, _dtype_code(k_out),
                                                  kp, ks, vp, vs, _stream(dev, stream)))
     _moved(k_out, v_out)
     return k_out, v_out
@@ -644,15 +648,15 @@ def vd_attention_mx4(cache, q, n_valid, rows=None, scale=None, out=None, workspa
     dev, dtype, shape = cache[0].device, q.dtype, (S, L, Hq, t, 2 * B)
     qp, qs = _rows_view(q, "q", shape, dtype, dev)
     code = _dtype_code(q)
-    n_h = _host_list(n_valid, S, "n_valid")
-    r_h = None if rows is None else _host_list(rows, S, "rows")
+    n_h, n_p = _host_list(n_valid, S, "n_valid")
+    r_h, r_p = _no_list if rows is None else _host_list(rows, S, "rows")
     sc = (2.0 * B) ** -0.5 if scale is None else float(scale)
     lib = load()
     with _on(dev, stream):
         if out is None:
             out = torch.empty(shape, dtype=dtype, device=dev)
         if workspace is None:
-            longest = max(n_h) if isinstance(n_h, ctypes.Array) else int(n_h.max())
+            longest = int(max(n_h))
             size = lib.vd_attention_mx4_workspace_size(ctypes.byref(desc), code, t, min(max(longest, 0), desc.capacity))
             ws_p = None
             if size:
@@ -663,7 +667,7 @@ def vd_attention_mx4(cache, q, n_valid, rows=None, scale=None, out=None, workspa
             ws_p, size = workspace.data_ptr(), workspace.numel()
         op, os_ = _rows_view(out, "out", shape, dtype, dev)
         _check("vd_attention_mx4", lib.vd_attention_mx4(
-            ctypes.byref(desc), code, qp, qs, t, _ptr(r_h), sc, _ptr(n_h), op, os_, ws_p, size, _stream(dev, stream)))
+            ctypes.byref(desc), code, qp, qs, t, r_p, sc, n_p, op, os_, ws_p, size, _stream(dev, stream)))
     _moved(out)
     return out
 
@@ -674,8 +678,8 @@ def vd_evict_step_mx4(cache, n_valid, budget, variant="l2", pos=None, scores_out
     desc = mx4_desc(cache)
     S, L, H, C, _ = cache[0].shape
     dev, U = cache[0].device, S * L * H
-    n_h = _host_list(n_valid, S, "n_valid")
-    b_h = _host_list(budget, S, "budget")
+    n_h, n_p = _host_list(n_valid, S, "n_valid")
+    b_h, b_p = _host_list(budget, S, "budget")
     if pos is not None:
         _need(pos, "pos", torch.int32, U * C, dev)
     if scores_out is not None:
@@ -684,7 +688,7 @@ def vd_evict_step_mx4(cache, n_valid, budget, variant="l2", pos=None, scores_out
         _need(keep_out, "keep_out", torch.uint8, U * C, dev)
     with _on(dev, stream):
         _check("vd_evict_step_mx4", load().vd_evict_step_mx4(
-            ctypes.byref(desc), _ptr(n_h), _ptr(b_h), VARIANTS[variant], _ptr(pos), _ptr(scores_out), _ptr(keep_out),
+            ctypes.byref(desc), n_p, b_p, VARIANTS[variant], _ptr(pos), _ptr(scores_out), _ptr(keep_out),
             _stream(dev, stream)))
     _moved(*cache, *(x for x in (pos, scores_out, keep_out) if x is not None))
 

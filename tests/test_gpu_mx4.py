@@ -560,3 +560,48 @@ def test_other_streams():
     stream.synchronize()
     assert all(torch.equal(x, want) for x in outs)
     assert torch.equal(rows[0].cpu().double(), ref.decode(cache.k, cache.k_scale)[:, :, :, :10])
+
+
+def test_binding_arguments():
+    """Counts as lists, tuples, tensors or numpy numbers; what does not fit is refused with nothing changed."""
+    import numpy as np
+    cache = _cache(2, 1, 2, 40, 64, 121)
+    q = _rows((2, 1, 4, 3, 64), torch.bfloat16, 122, 0.3).to(DEV)
+    want = vd.vd_attention_mx4(cache, q, [40, 17])
+    for n in ((40, 17), torch.tensor([40, 17]), torch.tensor([40, 17], device=DEV), [np.int64(40), np.int32(17)], np.array([40, 17])):
+        assert torch.equal(vd.vd_attention_mx4(cache, q, n), want)
+    rows = torch.zeros((2, 1, 2, 5, 64), device=DEV)
+    before = [x.clone() for x in cache]
+    pos = torch.zeros((4, 40), dtype=torch.int32, device=DEV)
+    for call in (lambda: vd.vd_append_mx4(cache, [0], rows, rows), lambda: vd.vd_append_mx4(cache, [36, 0], rows, rows),
+                 lambda: vd.vd_append_mx4(cache, [0, 0], rows, rows.bfloat16()), lambda: vd.vd_append_mx4(cache, [0, 0], rows.double(), rows.double()),
+                 lambda: vd.vd_append_mx4(cache, [0, 0], rows[:, :, :1], rows), lambda: vd.vd_append_mx4(cache, [0, 0], rows.cpu(), rows),
+                 lambda: vd.vd_append_mx4(cache, [0, 0], rows[0], rows[0]), lambda: vd.vd_append_mx4(cache, [0, 2 ** 31], rows, rows),
+                 lambda: vd.vd_append_mx4(cache, [0, 0], rows.transpose(3, 4), rows), lambda: vd.vd_append_mx4(cache, [0, 0.5], rows, rows[:1]),
+                 lambda: vd.vd_append_mx4(cache, [0, 0], rows, rows, pos=pos.long()), lambda: vd.vd_append_mx4(cache, [0, 0], rows, rows, [6, 0]),
+                 lambda: vd.vd_append_mx4(cache, [0, 0], rows[:, :, :, :0], rows[:, :, :, :0]),
+                 lambda: vd.vd_evict_step_mx4(cache, [41, 1], [4, 4]), lambda: vd.vd_evict_step_mx4(cache, [40, 1], [4, 0]),
+                 lambda: vd.vd_evict_step_mx4(cache, [40, 1], [4, 4], keep_out=pos), lambda: vd.vd_evict_step_mx4(cache, [40, 1], [4, 4], "fastcaote"),
+                 lambda: vd.vd_attention_mx4(cache, q[:1], [4, 4]), lambda: vd.vd_attention_mx4(cache, q[:, :, :3], [4, 4]),
+                 lambda: vd.vd_attention_mx4(cache, q.half(), [4, 4]), lambda: vd.vd_attention_mx4(cache, q, [4, 4], out=q),
+                 lambda: vd.vd_attention_mx4(cache, q, [4, 4], scale=math.inf), lambda: vd.vd_attention_mx4(cache, q, [4, 4], out=q.float()),
+                 lambda: vd.vd_attention_mx4(cache, q.detach().clone().requires_grad_(), [4, 4])):
+        with pytest.raises((ValueError, TypeError, RuntimeError)):   # (torch's own, or vd.VdError)
+            call()
+    torch.cuda.synchronize()
+    assert all(torch.equal(x, y) for x, y in zip(cache, before))
+
+
+def test_versions_move():
+    """torch's backward notices a cache that was written since it was saved; inference tensors are taken too."""
+    cache = _cache(1, 1, 1, 9, 64, 123)
+    rows = torch.ones((1, 1, 1, 1, 64), device=DEV)
+    before = [x._version for x in cache]
+    vd.vd_append_mx4(cache, [8], rows, rows)
+    vd.vd_evict_step_mx4(cache, [9], [8])
+    assert all(x._version > v for x, v in zip(cache, before))
+    with torch.inference_mode():
+        frozen = vd.Mx4Cache(*(x.clone() for x in cache))
+        vd.vd_append_mx4(frozen, [8], rows, rows)
+        inside = vd.vd_attention_mx4(frozen, rows, [9])
+    assert torch.equal(vd.vd_attention_mx4(frozen, rows, [9]), inside)
