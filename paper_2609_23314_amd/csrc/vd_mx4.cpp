@@ -174,7 +174,11 @@ AttnPlan attn_plan(const vd_mx4_cache *c, int32_t dtype, int64_t max_rows, int64
     a.block = queries > 4 * vd::kMxTile && !(dtype == VD_DTYPE_F32 && c->head_dim == 256);
     const int64_t tile = a.block ? vd::kMxBlockTile : vd::kMxTile;
     a.tiles = int((queries + tile - 1) / tile);
-    const int64_t groups = units * a.tiles, resident = (a.block ? vd::block_groups(dtype, c->head_dim) : 4) * 256;
+    // Splits where the launch has fewer workgroups than the CUs hold: as many as make two on
+    // each (of blocks, as many as are resident).  More cost the join what they save (one
+    // sequence of 131072 rows, 8 units, two and four workgroups a CU 33.9 and 36.2 us; sixteen
+    // of up to 4097, 128 units, 17.6 and 17.8, eight 19.0).
+    const int64_t groups = units * a.tiles, resident = (a.block ? vd::block_groups(dtype, c->head_dim) : 2) * 256;
     a.splits = int(std::max<int64_t>(1, std::min<int64_t>({vd::kMxMaxSplits, resident / groups, n / 256})));
     return a;
 }
