@@ -407,9 +407,11 @@ vd_status vd_read_mx4(const vd_mx4_cache *cache, const int32_t *first, const int
  *              left as they were.  Must not overlap q or the cache.
  *   workspace  device, 16-byte aligned, at least vd_attention_mx4_workspace_size()
  *              bytes (may be NULL when that is 0); calls that share one must not overlap
- * Logits, softmax and sums are fp32, products exact; a weight is rounded to bf16
- * (2^-8 of it) for bf16 queries and to two bf16 parts (2^-16) for fp32 ones.  A cached
- * row with a NaN group makes NaN of the outputs that see it, and of no other.
+ * Logits, softmax and sums are fp32.  Products are exact, but that in blocks of
+ * bf16 queries a query's channel is held to 2^-21 of the largest of its 32.  A
+ * weight is rounded to bf16 (2^-8 of it) for bf16 queries and to two bf16 parts
+ * (2^-16) for fp32 ones.  A cached row with a NaN group makes NaN of the outputs
+ * that see it, and of no other.
  */
 vd_status vd_attention_mx4(const vd_mx4_cache *cache, int32_t dtype, const void *q,
                            const int64_t *q_strides, int32_t max_rows, const int32_t *rows, float scale,
@@ -442,8 +444,9 @@ vd_status vd_evict_step_mx4(const vd_mx4_cache *cache, const int32_t *n_valid, c
  *   (y_a cos t - y_b sin t, y_b cos t + y_a sin t), t = pos * inv_freq[i],
  *   with (a, b) = (i, i + rotary/2), or (2i, 2i + 1) where interleaved;
  *   channels from `rotary` on are not rotated.
- * Either side may be left out (its x and out NULL).  fp32 arithmetic, the angle in
- * fp64, one rounding at the end.
+ * Either side may be left out (its x and out NULL); no row of one side is a row of
+ * the other (both may be parts of one projection's rows).  fp32 arithmetic, the angle
+ * in fp64, one rounding at the end.
  */
 typedef struct {
     const void *x;             /* device; row i of (seq, layer, head) by `strides` */

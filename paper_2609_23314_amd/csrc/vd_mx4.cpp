@@ -303,14 +303,19 @@ extern "C" vd_status vd_evict_step_mx4(const vd_mx4_cache *cache, const int32_t 
             }
         }
         if (!any) continue;
-        // More units than CUs: two workgroups of half the threads on a CU, so that one's
-        // selection and gather run beside another's rows.
-        p.threads = units * ns > 256 ? vd::kMxEvictThreads / 2 : vd::kMxEvictThreads;
-        // keys (the sums' partials lie there before them), then two lists of 16-bit slots
-        const int64_t partial = int64_t(p.threads / 64) * cache->head_dim * 8;
-        p.off_lists = int32_t(std::max(align16(int64_t(keys) * 4), partial));
-        p.list_cap = moves;
-        const size_t lds = size_t(p.off_lists + align16(int64_t(moves) * 4));
+        // Keys (the sums' partials lie there before them), then two lists of 16-bit slots.
+        // More units than CUs: two workgroups of half the threads on a CU, if its LDS holds
+        // both (12 KB each beside this), so that one's selection and gather run beside
+        // another's rows (1024 units of 4097 rows, one evicted, 154 and 124 us).
+        size_t lds = 0;
+        for (int threads : {vd::kMxEvictThreads / 2, vd::kMxEvictThreads}) {
+            const int64_t partial = int64_t(threads / 64) * cache->head_dim * 8;
+            p.threads = threads;
+            p.off_lists = int32_t(std::max(align16(int64_t(keys) * 4), partial));
+            p.list_cap = moves;
+            lds = size_t(p.off_lists + align16(int64_t(moves) * 4));
+            if (units * ns > 256 && lds + 12 * 1024 <= 80 * 1024) break;
+        }
         st = launched(vd::launch_mx_evict(p, ns, cache->head_dim, lds, reinterpret_cast<hipStream_t>(stream)));
         if (st != VD_OK) return st;
     }
