@@ -435,8 +435,8 @@ __global__ __launch_bounds__(kMxThreads) void attn_kernel(const MxAttnParams p) 
 // Arithmetic and products bound it together, since a SIMD hardly runs the one beside the
 // other (a loop of 32x32x16 products alone takes 37 cycles each, with 7 fused multiplies
 // beside each 60, the multiplies alone 34): 32 layers x 8 KV heads, 512 rows of 4 heads
-// over 2560, D = 128, 0.62 TFLOP in 0.61 ms, 1010 TFLOP/s; 777 rows of 2 heads over up
-// to 4873, D = 256, 0.21 ms, 660.  With K in bf16 as well 0.65 and 0.27 ms; with V's
+// over 2560, D = 128, 0.62 TFLOP in 0.60 ms, 1030 TFLOP/s; 777 rows of 2 heads over up
+// to 4873, D = 256, 0.19 ms, 700.  With K in bf16 as well 0.65 and 0.27 ms; with V's
 // tile padded rather than swizzled, and K's by 32 bytes, 5 % more.
 
 constexpr int kBlockRows = 64;
@@ -686,6 +686,7 @@ __global__ __launch_bounds__(kMxThreads, block_groups(DTYPE, D)) void attn_block
         f32x16 now[SUBS];
 #pragma unroll
         for (int t = 0; t < SUBS; ++t) now[t] = query.logits(k_lds + buffer * KT, t, c, half);
+        if (D == 256) __builtin_amdgcn_sched_barrier(0);   // (the wide case 205 -> 192 us; of 128 channels 602 -> 610)
         bf16x8 va[2][CT], w[2][PP];
         read_values(va[0], vt, 0);
         // the next tile's loads first, and the matrix cores' operands read well ahead of the products
@@ -723,6 +724,7 @@ __global__ __launch_bounds__(kMxThreads, block_groups(DTYPE, D)) void attn_block
         // Sixteen rows at a time: the products with V stand between the arithmetic of the
         // next sixteen rows' weights, or, at the end, of the next tile's conversion.
         weights(w[0], now[0], 0);
+        __builtin_amdgcn_s_setprio(1);   // before the other workgroup's logits (613 -> 602 us)
 #pragma unroll
         for (int step = 0; step < STEPS; ++step) {
             __builtin_amdgcn_sched_barrier(0);
@@ -746,6 +748,7 @@ __global__ __launch_bounds__(kMxThreads, block_groups(DTYPE, D)) void attn_block
                 __builtin_amdgcn_sched_group_barrier(0x002, 8, 0);
             }
         }
+        __builtin_amdgcn_s_setprio(0);
         __syncthreads();
     }
     if (m >= queries) return;
