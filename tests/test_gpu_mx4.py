@@ -605,3 +605,61 @@ def test_versions_move():
         vd.vd_append_mx4(frozen, [8], rows, rows)
         inside = vd.vd_attention_mx4(frozen, rows, [9])
     assert torch.equal(vd.vd_attention_mx4(frozen, rows, [9]), inside)
+
+
+def test_calls_at_once():
+    """Split calls on two streams at a time over one cache, each with a workspace of its own."""
+    cache = _cache(1, 1, 2, 6000, 128, 131)
+    qs = [_rows((1, 1, 8, t, 128), torch.bfloat16, 132 + t, 0.3).to(DEV) for t in (1, 50)]
+    want = [vd.vd_attention_mx4(cache, q, [6000]) for q in qs]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in qs]
+    outs = [[vd.vd_attention_mx4(cache, q, [6000], stream=s) for q, s in zip(qs, streams)] for _ in range(10)]
+    torch.cuda.synchronize()
+    assert all(torch.equal(x, y) for pair in outs for x, y in zip(pair, want))
+
+
+def test_graph_of_a_block():
+    """A prompt block in a graph: rotation in place, append, attention split over few units, eviction;
+    every replay against the eager calls, eager work between them."""
+    H, G, D, N, t = 1, 2, 128, 2500, 70
+    a, b = [Mx4EvictingCache(1, 1, H, D, N + t, [N], device=DEV) for _ in range(2)]
+    fill = [_rows((1, 1, H, N, D), torch.bfloat16, 600 + i).to(DEV) for i in (0, 1)]
+    for c in (a, b):
+        c.append(*fill)
+    ins = [[torch.zeros((1, 1, x, t, D), dtype=torch.bfloat16, device=DEV) for x in (G * H, H, H)] for _ in (a, b)]
+    pos = torch.arange(N, N + t, dtype=torch.int32, device=DEV).view(1, t)
+    inv_freq = (10000.0 ** (-torch.arange(0, D, 2).double() / D)).float().to(DEV)
+    w = torch.ones(1, D, device=DEV)
+
+    def step(c, x):
+        c.n, c.seen = [N], [N]
+        q, k, v = x
+        vd.vd_qk_norm_rope(q, k, pos, inv_freq, w, w, q, k)
+        c.append(k, v)
+        out = c.attend(q)
+        c.evict()
+        return out
+
+    assert vd.vd_attention_mx4_workspace_size(a.cache, H * G, t) > 0
+    saved = [x.clone() for x in (*a.cache, a.pos)]
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        step(a, ins[0])
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        captured = step(a, ins[0])
+    for x, y in zip((*a.cache, a.pos), saved):
+        x.copy_(y)
+    for r in range(4):
+        for i in range(3):
+            new = _rows(ins[0][i].shape, torch.bfloat16, 700 + 10 * r + i, 0.3)
+            ins[0][i].copy_(new)
+            ins[1][i].copy_(new)
+        graph.replay()
+        torch.cuda.synchronize()
+        want = step(b, ins[1])
+        torch.cuda.synchronize()
+        assert torch.equal(captured, want) and torch.isfinite(want).all()
+        assert all(torch.equal(x, y) for x, y in zip((*a.cache, a.pos), (*b.cache, b.pos)))
